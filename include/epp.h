@@ -306,6 +306,88 @@ int epp_input_gradient(epp_paths_t* paths, int k, const float* grad_X, int F_out
 int epp_weight_gradient_static(epp_paths_t* paths, int k, const float* Y, int F_in, const float* grad_X, int F_out,
                                float* grad_W, epp_stream_t stream);
 
+/* ---- rows that belong to groups --------------------------------------------------------------
+ * A layer whose rows have different weight matrices: one per type of vertex, or per expert of a mixture.  The calls below are the
+ * combination stage of such a layer.  Entries 0 .. m-1 are kept in the order of their groups; group g holds the entries
+ * [offsets[g], offsets[g + 1]), offsets lying on the GPU, so that a router's choices need not be known to the host.  Everything
+ * only enqueues kernels on `stream` (no allocation, no host wait; may be captured in a HIP graph), and equal inputs give
+ * bit-identical results.  A workspace is scratch memory of one call at a time. */
+
+/* Element types of matrices and gradients. */
+#define EPP_FLOAT32 0
+#define EPP_BFLOAT16 1
+#define EPP_FLOAT16 2
+
+/* Entries in the order of their groups.  Entry i is the row rows[i] (rows == NULL: row i, n == m), its group is group_of[row].
+ *   group_of   device, n; a number outside [0, G): the row is in no group
+ *   rows       device, m, or NULL (for instance epp_active_set_export's: the active vertices by their type); a row outside
+ *              [0, n) is in no group, a row listed twice is two entries
+ *   G          1 .. 2048
+ *   offsets    device, G + 1: offsets[0] = 0, offsets[G]: entries that are in a group
+ *   order      device, m: the entries' rows, group by group and within a group in the order of the entries; from offsets[G] on
+ *              those in no group, in their order
+ *   workspace  device, at least epp_group_rows_workspace(m, G) bytes, 16-byte aligned */
+int64_t epp_group_rows_workspace(int64_t m, int G); /* bytes, < 0: error */
+int epp_group_rows(const int32_t* group_of, int64_t n, const int32_t* rows, int64_t m, int G, int32_t* offsets, int32_t* order,
+                   void* workspace, int64_t workspace_bytes, epp_stream_t stream);
+
+/* A matrix whose rows entries name: entry i is row rows[i], or row i where rows is NULL (n >= m then). */
+typedef struct {
+    void* data;          /* device, row-major                                                    */
+    int64_t n;           /* rows, < 2^31                                                         */
+    int64_t ld;          /* elements from row to row, at least the width                         */
+    const int32_t* rows; /* device, m; a row outside [0, n) counts as zeros and is never written */
+} epp_rows_t;
+
+/* Products of a layer with a weight matrix per group, entry i in group g:
+ *     epp_grouped_product           out[i, :]    = X[i, :] W[g]
+ *     epp_grouped_input_gradient    grad_X[i, :] = grad_out[i, :] W[g]^T
+ *     epp_grouped_weight_gradient   grad_W[g]    = sum over the entries i of group g of X[i, :]^T grad_out[i, :]
+ * where row i of a matrix means the row that entry i names.  Rows of out and grad_X that no entry of a group names are not
+ * touched; a row of them that two entries name receives one of the two, element by element, so name it once.  Rows of X and
+ * grad_out may be named any number of times.
+ *   type       of all matrices; sums are fp32, results are rounded to the type once
+ *   W          device, G x F_in x F_out, G matrices one after the other
+ *   offsets    device, G + 1, ascending within [0, m].  Entries below offsets[0] or from offsets[G] on take part in nothing.  Numbers
+ *              that are not as they should be give unspecified results, never an access outside the matrices.
+ *   grad_W     device, G x F_in x F_out of `type` or EPP_FLOAT32, overwritten (zeros for a group without entries)
+ *   workspace  device, at least epp_grouped_weight_gradient_workspace(...) bytes, 16-byte aligned: partial sums over blocks of
+ *              entries, which a second kernel adds in a fixed order
+ * 1 <= G <= 2048, 1 <= F_in, F_out <= 65,536, 0 <= m < 2^31.  Outputs must not alias inputs (columns of one wider matrix are fine). */
+int epp_grouped_product(int type, const epp_rows_t* X, const void* W, const int32_t* offsets, int G, int64_t m, int F_in, int F_out,
+                        const epp_rows_t* out, epp_stream_t stream);
+int epp_grouped_input_gradient(int type, const epp_rows_t* grad_out, const void* W, const int32_t* offsets, int G, int64_t m, int F_in,
+                               int F_out, const epp_rows_t* grad_X, epp_stream_t stream);
+int64_t epp_grouped_weight_gradient_workspace(int64_t m, int G, int F_in, int F_out); /* bytes, < 0: error */
+int epp_grouped_weight_gradient(int type, const epp_rows_t* X, const epp_rows_t* grad_out, const int32_t* offsets, int G, int64_t m,
+                                int F_in, int F_out, int grad_W_type, void* grad_W, void* workspace, int64_t workspace_bytes,
+                                epp_stream_t stream);
+
+/* ---- all gradients together ------------------------------------------------------------------ */
+
+/* One gradient of a model, of any shape: `count` consecutive elements. */
+typedef struct {
+    void* data;    /* device                                                                       */
+    void* out;     /* device: where epp_clip_gradients writes it (data itself: in place), or NULL: in place */
+    int64_t count; /* elements, >= 0                                                               */
+    int type;      /* EPP_FLOAT32, EPP_BFLOAT16, EPP_FLOAT16: of data and out                      */
+} epp_gradient_t;
+
+/* norm = sqrt(sum of x^2) over all elements of all n gradients, and (epp_clip_gradients) every gradient times
+ * min(1, max_norm / norm).  Squares are added in 64 bits, so no finite element's square overflows, and the norm is rounded to fp32
+ * once (beyond the largest float: infinity, and the gradients are scaled by the true value).  Gradients whose norm is not above
+ * max_norm keep their bits.  With a NaN among them norm and all scaled gradients are NaN; with an infinity the norm is infinite, the
+ * infinite elements become NaN and all others 0.  (max_norm = infinity: nothing is scaled but for NaN.)
+ *   grads      host, n of them (read during the call only), n <= 2^20; 0: the norm is 0
+ *   norm       device, one float
+ *   workspace  device, at least epp_gradient_norm_workspace(n) bytes, 16-byte aligned
+ * What is written must not overlap with anything else: a gradient listed twice is refused by epp_clip_gradients (and counts twice in
+ * epp_gradient_norm).  Enqueues only: one launch for the norm of up to 96 gradients, one to finish or to scale. */
+int64_t epp_gradient_norm_workspace(int n); /* bytes, < 0: error */
+int epp_gradient_norm(const epp_gradient_t* grads, int n, float* norm, void* workspace, int64_t workspace_bytes, epp_stream_t stream);
+int epp_clip_gradients(const epp_gradient_t* grads, int n, double max_norm, float* norm, void* workspace, int64_t workspace_bytes,
+                       epp_stream_t stream);
+
 void epp_destroy_paths(epp_paths_t* p);
 void epp_destroy_path(epp_path_t* p); /* only for handles from epp_prepare_full */
 

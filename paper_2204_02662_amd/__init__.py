@@ -33,6 +33,9 @@ EXPORTED = [
     "epp_last_error", "epp_paper_linreg_group_size", "epp_ifelse_aggregate",
     "epp_weight_gradient_workspace", "epp_weight_gradient", "epp_input_gradient", "epp_paths_import",
     "epp_path_prepare_width", "epp_weight_gradient_static",
+    "epp_group_rows_workspace", "epp_group_rows", "epp_grouped_product", "epp_grouped_input_gradient",
+    "epp_grouped_weight_gradient_workspace", "epp_grouped_weight_gradient",
+    "epp_gradient_norm_workspace", "epp_gradient_norm", "epp_clip_gradients",
 ]
 
 
@@ -45,6 +48,14 @@ class EppError(RuntimeError):
 class _Csr(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int64), ("nnz", ctypes.c_int64), ("rowptr", ctypes.c_void_p),
                 ("col", ctypes.c_void_p), ("val", ctypes.c_void_p)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("ld", ctypes.c_int64), ("rows", ctypes.c_void_p)]
+
+
+class _Gradient(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64), ("type", ctypes.c_int)]
 
 
 class _PathArrays(ctypes.Structure):
@@ -143,6 +154,19 @@ def load_library() -> ctypes.CDLL:
     lib.epp_weight_gradient_static.argtypes = [P, I, P, I, P, I, P, P]
     lib.epp_input_gradient.argtypes = [P, I, P, I, P, I, P, P]
     lib.epp_paths_import.argtypes = [I64, I, P, I64, ctypes.POINTER(_PathArrays), A, P, ctypes.POINTER(P)]
+    R = ctypes.POINTER(_Rows)
+    lib.epp_group_rows_workspace.argtypes = [I64, I]
+    lib.epp_group_rows_workspace.restype = I64
+    lib.epp_group_rows.argtypes = [P, I64, P, I64, I, P, P, P, I64, P]
+    lib.epp_grouped_product.argtypes = [I, R, P, P, I, I64, I, I, R, P]
+    lib.epp_grouped_input_gradient.argtypes = [I, R, P, P, I, I64, I, I, R, P]
+    lib.epp_grouped_weight_gradient_workspace.argtypes = [I64, I, I, I]
+    lib.epp_grouped_weight_gradient_workspace.restype = I64
+    lib.epp_grouped_weight_gradient.argtypes = [I, R, R, P, I, I64, I, I, I, P, P, I64, P]
+    lib.epp_gradient_norm_workspace.argtypes = [I]
+    lib.epp_gradient_norm_workspace.restype = I64
+    lib.epp_gradient_norm.argtypes = [ctypes.POINTER(_Gradient), I, P, P, I64, P]
+    lib.epp_clip_gradients.argtypes = [ctypes.POINTER(_Gradient), I, ctypes.c_double, P, P, I64, P]
     lib.epp_destroy_paths.argtypes = [P]
     lib.epp_destroy_paths.restype = None
     lib.epp_destroy_path.argtypes = [P]
@@ -336,8 +360,25 @@ def epp_weight_gradient_workspace(paths: Paths, k: int, F_in: int, F_out: int) -
     return _check(load_library().epp_weight_gradient_workspace(paths._h, k, F_in, F_out))
 
 
+def epp_group_rows_workspace(entries: int, G: int) -> int:
+    """Bytes of workspace for epp_group_rows."""
+    return _check(load_library().epp_group_rows_workspace(entries, G))
+
+
+def epp_grouped_weight_gradient_workspace(entries: int, G: int, F_in: int, F_out: int) -> int:
+    """Bytes of workspace for epp_grouped_weight_gradient."""
+    return _check(load_library().epp_grouped_weight_gradient_workspace(entries, G, F_in, F_out))
+
+
+def epp_gradient_norm_workspace(n: int) -> int:
+    """Bytes of workspace for epp_gradient_norm and epp_clip_gradients of n gradients."""
+    return _check(load_library().epp_gradient_norm_workspace(n))
+
+
 try:
-    from ._binding import (epp_backward_aggregate, epp_full_aggregate, epp_input_gradient, epp_weight_gradient,
+    from ._binding import (epp_backward_aggregate, epp_clip_gradients, epp_full_aggregate, epp_gradient_norm,
+                           epp_group_rows, epp_grouped_input_gradient, epp_grouped_product,
+                           epp_grouped_weight_gradient, epp_input_gradient, epp_weight_gradient,
                            epp_weight_gradient_static, alloc_news as _alloc_news, allocator as _native_allocator,
                            init as _init_binding)
     _init_binding(EppError, _raw_stream)
@@ -348,6 +389,8 @@ except ImportError as _e:  # not built yet: the package can be imported (to buil
         raise FileNotFoundError(f"{PKG}/_binding is not usable ({_why}): run `python -m paper_2204_02662_amd.build`")
     epp_backward_aggregate = epp_full_aggregate = epp_input_gradient = _not_built
     epp_weight_gradient = epp_weight_gradient_static = _not_built
+    epp_group_rows = epp_grouped_product = epp_grouped_input_gradient = epp_grouped_weight_gradient = _not_built
+    epp_gradient_norm = epp_clip_gradients = _not_built
 
     # (what goes through ctypes runs all the same, and on PyTorch's memory: NULL functions would be hipMalloc's)
     def _alloc_news(stats):
