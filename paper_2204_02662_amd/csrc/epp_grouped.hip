@@ -40,11 +40,13 @@ typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 
 constexpr int kMaxGroups = 2048;
 constexpr int kMaxWidth = 1 << 16;
-constexpr int kLine = 128;  // bytes of the contraction in a tile
+constexpr int kLine = 128;   // bytes of the contraction in a tile
+constexpr int kUnits = 256;  // compute units
 
 enum Mode { kProduct, kInput, kWeight };
 
 __device__ __attribute__((aligned(128))) unsigned int g_zeros[32] = {};
+__device__ int32_t g_none = -1;  // no row
 
 struct Side {           // a matrix and the rows of it that entries name
     const char* data;
@@ -58,7 +60,6 @@ struct GroupedArgs {
     const int32_t* offsets;
     int64_t m;
     int G, F_in, F_out;
-    int vec_out;        // results are written four at a time
     int64_t per;        // weight gradient: entries to a chunk (0: whole groups)
     float* part;        // .. and its partial sums
 };
@@ -90,6 +91,12 @@ __device__ __forceinline__ floatx16 multiply(uintx4 a, uintx4 b, floatx16 c) {
     }
 }
 
+// The same value in all lanes, and the compiler told so.
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+    return (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)x) | (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32);
+}
+__device__ __forceinline__ const char* uniform(const char* p) { return reinterpret_cast<const char*>(uniform(reinterpret_cast<int64_t>(p))); }
+
 // ---------------------------------------------------------------- groups
 struct Span { int g; int64_t first, last, chunk0; };  // a group (-1: none), its entries, its first tile
 
@@ -120,7 +127,7 @@ __device__ __forceinline__ Span find_group(const int32_t* __restrict__ offsets, 
         }
         before += __shfl(upto, 63, 64);
     }
-    *total = before;
+    *total = uniform(before);
     found.g = __builtin_amdgcn_readfirstlane(found.g);
     return found;
 }
@@ -134,6 +141,12 @@ __device__ __forceinline__ unsigned lds_address(const void* p) {
 __device__ __forceinline__ void load_to_lds(const char* from, unsigned to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
 }
+__device__ __forceinline__ void load4_to_lds(const char* from, unsigned to) {  // (4 bytes a lane)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory");
+}
+__device__ __forceinline__ void load_to_lds(const char* base, unsigned off, unsigned to) {  // (base the same in all lanes)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+}
 // All loads of this wavefront have arrived and all its LDS reads are done; then the same for the workgroup's.
 __device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
@@ -142,7 +155,7 @@ __device__ __forceinline__ int64_t row_of(const Side& s, int64_t i, bool valid) 
     const int64_t r = s.rows ? (int64_t)s.rows[i] : i;
     return r >= 0 && r < s.n ? r : -1;
 }
-
+__device__ __forceinline__ const char* zeros() { return reinterpret_cast<const char*>(g_zeros); }
 // A piece with `valid` elements (0 .. a piece's), through registers.
 template <class T>
 __device__ __forceinline__ uintx4 load_piece(const char* p, int64_t valid) {
@@ -162,40 +175,46 @@ __device__ __forceinline__ uintx4 load_piece(const char* p, int64_t valid) {
     return v;
 }
 
-// Lines of K: TD rows, row r's place set once.
+// Lines of K: TD rows, whose places are set once.  DIRECT: what stands in a line without a row is somebody's numbers (the result's row
+// is not written, or written as zeros); behind the contraction's end there are zeros.
 template <class T, int TD, int NT, bool DIRECT>
 struct LinesOfK {
-    static constexpr int E = 16 / (int)sizeof(T), N = TD * 8 / NT, kBytes = TD * kLine;
-    const char* p[N];
-    uint64_t bad = 0;  // bit i: piece i has no row
-    int k;             // element of the contraction where this thread's pieces begin
-    int K;
+    static constexpr int E = 16 / (int)sizeof(T), N = TD * 8 / NT, kBytes = TD * kLine, kSteps = kLine / (int)sizeof(T);
+    const char* base;  // DIRECT: the same for all lanes, moves with the contraction
+    unsigned off[DIRECT ? N : 1];
+    const char* p[DIRECT ? 1 : N];
     uintx4 held[DIRECT ? 1 : N];
-    // row(i): place of tile row i, null: none
-    template <class F> __device__ __forceinline__ void start(int K_, F row) {
+    int k, K;          // the contraction's element in this thread's pieces, and its end
+    unsigned lds_wave;
+    // place(i): place of tile row i as seen from `from`, -1: none
+    template <class F> __device__ __forceinline__ void start(const char* from, int end, int wave, F place) {
         const int t = threadIdx.x;
-        K = K_;
-        k = ((t & 7) ^ ((t >> 3) & 7)) * E;
+        K = end;
+        k = ((t & 7) ^ ((t >> 4) & 7)) * E;
+        base = uniform(from);
+        lds_wave = (unsigned)wave * 1024u;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            p[i] = row((i * NT + t) >> 3);
-            if (!p[i]) bad |= 1ull << i;
-            p[i] += (int64_t)k * (int64_t)sizeof(T);
+            const int64_t at = place((i * NT + t) >> 3);
+            if constexpr (DIRECT) off[i] = (unsigned)(at < 0 ? 0 : at) + (unsigned)k * (unsigned)sizeof(T);
+            else p[i] = at < 0 ? nullptr : from + at;
         }
     }
-    __device__ __forceinline__ void fetch(char* to) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const bool no = (bad >> i) & 1;
-            if constexpr (DIRECT) {
-                load_to_lds(no || k >= K ? reinterpret_cast<const char*>(g_zeros) : p[i],
-                            __builtin_amdgcn_readfirstlane(lds_address(to + (i * NT + (threadIdx.x & ~63)) * 16)));
-            } else {
-                held[i] = load_piece<T>(p[i], no ? 0 : K - k);
-            }
-            p[i] += kLine;
+    __device__ __forceinline__ void prepare() {}
+    // Piece i of the next tile, which the contraction fills (FULL), or as far as it goes.
+    template <bool FULL>
+    __device__ __forceinline__ void fetch(int i, char* to) {
+        if constexpr (DIRECT) {
+            const unsigned at = lds_address(to) + lds_wave + (unsigned)(i * NT * 16);
+            if (FULL) load_to_lds(base, off[i], at);
+            else load_to_lds(k < K ? base + off[i] : zeros(), at);
+        } else {
+            held[i] = load_piece<T>(p[i] + (int64_t)k * (int64_t)sizeof(T), p[i] ? K - k : 0);
         }
-        k += kLine / (int)sizeof(T);
+    }
+    __device__ __forceinline__ void advance() {  // after all pieces of a tile
+        base += kLine;
+        k += kSteps;
     }
     __device__ __forceinline__ void put(char* to) {
         if constexpr (!DIRECT) {
@@ -206,59 +225,115 @@ struct LinesOfK {
     // Piece 2 s + half of rows c0 + l % 32 (c0 a multiple of 32).
     static __device__ __forceinline__ uintx4 piece(const char* tile, int c0, int s) {
         const int l = threadIdx.x & 63;
-        return *reinterpret_cast<const uintx4*>(tile + (c0 + (l & 31)) * kLine + (((2 * s + (l >> 5)) ^ (l & 7)) * 16));
+        return *reinterpret_cast<const uintx4*>(tile + (c0 + (l & 31)) * kLine + (((2 * s + (l >> 5)) ^ ((l >> 1) & 7)) * 16));
     }
 };
 
-// Lines of width: the steps of the contraction are the entries [first, last) of `s`, the columns begin at c0.
-template <class T, int TD, int NT, bool DIRECT>
+// Lines of width: the steps of the contraction are the entries [first, last) of `s`, the columns begin at c0.  LIST: the entries may name
+// rows through a list.
+template <class T, int TD, int NT, bool DIRECT, bool LIST>
 struct LinesOfWidth {
     static constexpr int E = 16 / (int)sizeof(T), N = TD * 8 / NT, kBytes = TD * kLine;
-    static constexpr int kWide = TD * (int)sizeof(T), kPieces = kWide / 16, kUnits = kWide / 32, kMask = (kUnits < 8 ? kUnits : 8) - 1;
+    static constexpr int kWide = TD * (int)sizeof(T), kPieces = kWide / 16, kPairs = kWide / 32;
     static constexpr int kSteps = kLine / (int)sizeof(T);
-    static_assert(NT % kPieces == 0 && (kMask & (kMask + 1)) == 0, "tile");
-    Side s;
-    int64_t at, last;   // entry of this thread's first piece in the next tile
-    int32_t row[N];     // rows of the next tile's pieces where there is a list of them
-    int col, width;
-    uintx4 held[DIRECT ? 1 : N];
-    __device__ __forceinline__ int column(int i) const {  // of this thread's piece i, in elements
-        const int t = threadIdx.x, line = (i * NT + t) / kPieces;
-        return col + (((t % kPieces) ^ ((line & kMask) << 1)) * E);
+    static_assert(NT % kPieces == 0 && (kPairs == 4 || kPairs % 8 == 0), "tile");
+    // What a line's units of 32 bytes are permuted by.
+    static __device__ __forceinline__ int turn(int line) {
+        if constexpr (sizeof(T) == 4) return ((line >> 2) & 1) << 2;
+        else if constexpr (kPairs == 4) return ((line >> 1) & 1) << 1;
+        else return (line & 3) << 1;
     }
-    __device__ __forceinline__ void start(const Side& side, int64_t first, int64_t end, int c0, int w) {
+    static constexpr int kLines = NT / kPieces;  // lines from piece to piece of a thread
+    static_assert(kLines % 8 == 0, "all of a thread's pieces are of the same columns");
+    Side s;
+    int64_t at, last;   // entry of this thread's first piece in the next tile, and the end
+    int c, width;       // column of this thread's pieces; columns
+    const char* base;   // DIRECT, no list: place of the next tile's first line, the same for all lanes
+    unsigned off;       // .. and of this thread's first piece, seen from there
+    const char* col;    // DIRECT, list: place of column c of row 0
+    const char* p[DIRECT && LIST ? N : 1];  // .. places of the next tile's pieces
+    char* ring;         // .. four tiles' rows in LDS, each 64 of them: arrived two tiles before they are used
+    int64_t ask;        // .. entry where the next tile to ask for begins, the same for all lanes
+    int slot;           // .. place in the ring of the next tile
+    bool asks;          // .. this wavefront loads the list
+    int32_t row[!DIRECT && LIST ? N : 1];
+    unsigned lds_wave;
+    uintx4 held[DIRECT ? 1 : N];
+    __device__ __forceinline__ void start(const Side& side, int64_t first, int64_t end, int c0, int w, int wave, char* lds_ring = nullptr, bool loads_list = false) {
+        const int t = threadIdx.x, line = t / kPieces;
         s = side;
-        at = first + threadIdx.x / kPieces;
+        at = first + line;
         last = end;
-        col = c0;
         width = w;
-        next_rows();
+        c = c0 + ((t % kPieces) ^ (turn(line) << 1)) * E;
+        lds_wave = (unsigned)wave * 1024u;
+        if constexpr (DIRECT) {
+            if (c >= width) c = 0;  // (somebody's numbers, for a result that is not written)
+            base = uniform(s.data + first * s.ld);
+            off = (unsigned)line * (unsigned)s.ld + (unsigned)c * (unsigned)sizeof(T);
+            col = s.data + (int64_t)c * (int64_t)sizeof(T);
+        }
+        if constexpr (LIST && DIRECT) {
+            ring = lds_ring;
+            ask = uniform(first);
+            slot = 0;
+            asks = loads_list;
+            ask_rows(0);
+            ask_rows(1);
+        }
+        if constexpr (LIST && !DIRECT) next_rows();
+    }
+    // The rows of a tile into slot q of the ring.  (Loaded into registers and kept there from tile to tile, they would have to be waited for
+    // behind the operands' loads, which the compiler's count of loads does not know: 594 instead of 380 us for 16 groups of 2,048 entries
+    // and 2,048 x 2,048 weights.)
+    __device__ __forceinline__ void ask_rows(int q) {
+        if (asks) {
+            const int64_t e = ask + (threadIdx.x & 63);
+            if (s.rows) load4_to_lds(reinterpret_cast<const char*>(e < last ? s.rows + e : &g_none), lds_address(ring) + (unsigned)q * 256u);
+            else reinterpret_cast<int32_t*>(ring + q * 256)[threadIdx.x & 63] = e < last ? (int32_t)e : -1;
+        }
+        ask += kSteps;
     }
     __device__ __forceinline__ void next_rows() {
         if (!s.rows) return;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int64_t e = at + i * (NT / kPieces);
-            row[i] = e < last ? s.rows[e] : -1;
-        }
+        for (int i = 0; i < N; ++i) row[i] = at + i * kLines < last ? s.rows[at + i * kLines] : -1;
     }
-    __device__ __forceinline__ void fetch(char* to) {
+    // The next tile's places.
+    __device__ __forceinline__ void prepare() {
+        if constexpr (DIRECT && LIST) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int64_t e = at + i * (NT / kPieces);
-            const int64_t r = s.rows ? (int64_t)row[i] : e;
-            const int c = column(i);
-            const bool no = e >= last || r < 0 || r >= s.n || c >= width;
-            const char* p = s.data + r * s.ld + (int64_t)c * (int64_t)sizeof(T);
-            if constexpr (DIRECT) {
-                load_to_lds(no ? reinterpret_cast<const char*>(g_zeros) : p,
-                            __builtin_amdgcn_readfirstlane(lds_address(to + (i * NT + (threadIdx.x & ~63)) * 16)));
-            } else {
-                held[i] = load_piece<T>(p, no ? 0 : width - c);
+            for (int i = 0; i < N; ++i) {
+                const uint32_t r = *reinterpret_cast<const uint32_t*>(ring + slot * 256 + (i * kLines + threadIdx.x / kPieces) * 4);
+                p[i] = r < (uint32_t)s.n ? col + (uint64_t)r * (uint64_t)(uint32_t)s.ld : zeros();
             }
         }
+    }
+    template <bool FULL>
+    __device__ __forceinline__ void fetch(int i, char* to) {
+        if constexpr (DIRECT) {
+            const unsigned lds = lds_address(to) + lds_wave + (unsigned)(i * NT * 16);
+            if constexpr (LIST) load_to_lds(p[i], lds);
+            else if (FULL) load_to_lds(base + (int64_t)(i * kLines) * s.ld, off, lds);
+            else load_to_lds(at + i * kLines < last ? base + (int64_t)(i * kLines) * s.ld + off : zeros(), lds);
+        } else {
+            const int64_t e = at + i * kLines;
+            int64_t r = e;
+            if constexpr (LIST) {
+                if (s.rows) r = row[i];
+            }
+            const bool no = e >= last || r < 0 || r >= s.n || c >= width;
+            held[i] = load_piece<T>(s.data + r * s.ld + (int64_t)c * (int64_t)sizeof(T), no ? 0 : width - c);
+        }
+    }
+    __device__ __forceinline__ void advance() {
         at += kSteps;
-        next_rows();
+        if constexpr (DIRECT) base += kSteps * s.ld;
+        if constexpr (DIRECT && LIST) {
+            ask_rows((slot + 2) & 3);
+            slot = (slot + 1) & 3;
+        }
+        if constexpr (!DIRECT && LIST) next_rows();
     }
     __device__ __forceinline__ void put(char* to) {
         if constexpr (!DIRECT) {
@@ -275,15 +350,15 @@ struct LinesOfWidth {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int line = 4 * q + j;
-                v[j] = *reinterpret_cast<const unsigned int*>(tile + line * kWide + (((x >> 3) ^ (line & kMask)) * 32) + (x & 7) * 4);
+                v[j] = *reinterpret_cast<const unsigned int*>(tile + line * kWide + (((x >> 3) ^ turn(line)) * 32) + (x & 7) * 4);
             }
             return v;
         } else {
             typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
             const int i = l & 15, unit = (c >> 4) + ((l >> 4) & 1);
             const int l0 = 8 * q + (i >> 2), l1 = l0 + 4;
-            const char* p0 = tile + l0 * kWide + ((unit ^ (l0 & kMask)) * 32) + (i & 3) * 8;
-            const char* p1 = tile + l1 * kWide + ((unit ^ (l1 & kMask)) * 32) + (i & 3) * 8;
+            const char* p0 = tile + l0 * kWide + ((unit ^ turn(l0)) * 32) + (i & 3) * 8;
+            const char* p1 = tile + l1 * kWide + ((unit ^ turn(l1)) * 32) + (i & 3) * 8;
             const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(p0));
             const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(p1));
             return __builtin_bit_cast(uintx4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -291,143 +366,227 @@ struct LinesOfWidth {
     }
 };
 
-// Four neighbouring results of a row; `valid` of them exist.
+// Four neighbouring results of a row; `valid` of them exist.  (A store needs no alignment beyond the element's.)
 template <class T>
-__device__ __forceinline__ void store4(char* row, int col, const float (&x)[4], int valid, bool vec) {
+__device__ __forceinline__ void store4(char* row, int col, const float (&x)[4], int valid) {
     T* p = reinterpret_cast<T*>(row) + col;
-    if (vec && valid >= 4) {
-        typedef T vec4 __attribute__((ext_vector_type(4)));
+    if (valid >= 4) {
+        typedef T vec4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
         *reinterpret_cast<vec4*>(p) = vec4{Num<T>::from(x[0]), Num<T>::from(x[1]), Num<T>::from(x[2]), Num<T>::from(x[3])};
     } else {
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+        for (int c = 0; c < 3; ++c)
             if (c < valid) p[c] = Num<T>::from(x[c]);
     }
 }
 
-// WM x WN wavefronts, each with BM x BN blocks of 32 x 32 of the result.  TO: type of the results.
-template <class T, class TO, int MODE, int WM, int WN, int BM, int BN, bool DIRECT>
-__global__ __launch_bounds__(64 * WM * WN) void k_grouped(GroupedArgs g) {
+// Where a tile of the result is.
+struct Place {
+    int g;                  // group (product, input gradient)
+    int64_t m0, m_end;      // rows of the result: entries, or rows of grad_W
+    int n0;
+    int64_t first, last;    // weight gradient: entries
+    char* out;              // .. and its matrix
+};
+
+// One tile: WM x WN wavefronts, each with BM x BN blocks of 32 x 32 of the result.  TO: type of the results.
+template <class T, class TO, int MODE, int WM, int WN, int BM, int BN, bool DIRECT, bool LIST>
+__device__ __forceinline__ void form_tile(const GroupedArgs& g, const Place& at, char* lds) {
     constexpr int NT = 64 * WM * WN, TM = 32 * WM * BM, TN = 32 * WN * BN;
-    using A = std::conditional_t<MODE == kWeight, LinesOfWidth<T, TM, NT, DIRECT>, LinesOfK<T, TM, NT, DIRECT>>;
-    using B = std::conditional_t<MODE == kInput, LinesOfK<T, TN, NT, DIRECT>, LinesOfWidth<T, TN, NT, DIRECT>>;
-    __shared__ __attribute__((aligned(128))) char tiles[2][A::kBytes + B::kBytes];
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = w % WM, wn = w / WM;
+    using A = std::conditional_t<MODE == kWeight, LinesOfWidth<T, TM, NT, DIRECT, LIST>, LinesOfK<T, TM, NT, DIRECT>>;
+    using B = std::conditional_t<MODE == kInput, LinesOfK<T, TN, NT, DIRECT>, LinesOfWidth<T, TN, NT, DIRECT, LIST>>;
+    constexpr int kBytes = A::kBytes + B::kBytes, kSteps = kLine / (int)sizeof(T);
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wn = w % WN, wm = w / WN;
     A a;
     B b;
-    int64_t K;                        // steps of the contraction
-    int64_t m0 = 0, m_end = 0;        // rows of the result: entries (product, input gradient) or rows of grad_W
-    int n0;
-    const int N = MODE == kInput ? g.F_in : g.F_out;
-    const int nt = (N + TN - 1) / TN;
-    char* out_base = const_cast<char*>(g.out.data);
+    int64_t K;  // steps of the contraction
+    const int64_t m0 = at.m0, m_end = at.m_end;
+    const int n0 = at.n0, N = MODE == kInput ? g.F_in : g.F_out;
     if constexpr (MODE != kWeight) {
-        // Workgroups b, b + 8, .. run on one XCD: it gets neighbouring tiles, which share rows and weights in its L2.
-        int64_t total;
-        Span s = find_group(g.offsets, g.G, g.m, TM, -1, &total);
-        const int64_t per = (total * nt + 7) / 8, mine = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-        if ((int64_t)(blockIdx.x >> 3) >= per || mine >= total * nt) return;
-        s = find_group(g.offsets, g.G, g.m, TM, mine / nt, &total);
-        m0 = s.first + (mine / nt - s.chunk0) * TM;
-        m_end = s.last;
-        n0 = (int)(mine % nt) * TN;
-        const int64_t w_bytes = (int64_t)g.F_in * g.F_out * (int64_t)sizeof(T);
-        const char* W = g.W + s.g * w_bytes;
+        const char* W = g.W + at.g * ((int64_t)g.F_in * g.F_out * (int64_t)sizeof(T));
         const int64_t ldw = (int64_t)g.F_out * (int64_t)sizeof(T);
         K = MODE == kInput ? g.F_out : g.F_in;
-        a.start((int)K, [&](int i) -> const char* {
+        // (with a list a row's place is counted from the first one, else from the tile's)
+        a.start(g.a.rows ? g.a.data : g.a.data + m0 * g.a.ld, (int)K, w, [&](int i) -> int64_t {
             const int64_t r = row_of(g.a, m0 + i, m0 + i < m_end);
-            return r < 0 ? nullptr : g.a.data + r * g.a.ld;
+            return r < 0 ? -1 : (g.a.rows ? r : (int64_t)i) * g.a.ld;
         });
-        if constexpr (MODE == kInput) {
-            b.start((int)K, [&](int i) -> const char* { return n0 + i < N ? W + (int64_t)(n0 + i) * ldw : nullptr; });
-        } else {
-            b.start(Side{W, K, ldw, nullptr}, 0, K, n0, N);
-        }
+        if constexpr (MODE == kInput) b.start(W + n0 * ldw, (int)K, w, [&](int i) -> int64_t { return n0 + i < N ? i * ldw : -1; });
+        else b.start(Side{W, K, ldw, nullptr}, 0, K, n0, N, w);
     } else {
-        const int mt = (g.F_in + TM - 1) / TM;
-        // (the tiles of one group or chunk are dealt to all XCDs: groups differ in size)
-        const int per_group = mt * nt, in = (int)(blockIdx.x % per_group), share = (per_group + 7) / 8;
-        const int64_t chunk = blockIdx.x / per_group;
-        int tile = in;
-        if (per_group % 8 == 0) tile = (in & 7) * share + (in >> 3);
-        int64_t first, last;
-        if (g.per) {
-            int64_t total;
-            const Span s = find_group(g.offsets, g.G, g.m, g.per, chunk, &total);
-            if (s.g < 0) return;
-            first = s.first + (chunk - s.chunk0) * g.per;
-            last = min(first + g.per, s.last);
-            out_base = reinterpret_cast<char*>(g.part + chunk * g.F_in * g.F_out);
-        } else {
-            first = min(max((int64_t)g.offsets[chunk], (int64_t)0), g.m);
-            last = max(first, min((int64_t)g.offsets[chunk + 1], g.m));
-            out_base += chunk * g.F_in * g.F_out * (int64_t)sizeof(TO);
-        }
-        K = last - first;
-        m0 = (int64_t)(tile / nt) * TM;
-        m_end = g.F_in;
-        n0 = (tile % nt) * TN;
-        a.start(g.a, first, last, (int)m0, g.F_in);
-        b.start(g.b, first, last, n0, g.F_out);
+        K = at.last - at.first;
+        char* ring = lds + 2 * kBytes;
+        a.start(g.a, at.first, at.last, (int)m0, g.F_in, w, ring, w == 0);
+        b.start(g.b, at.first, at.last, n0, g.F_out, w, ring + 1024, w == 1);
+        if (DIRECT && LIST) wait_and_meet();
     }
 
+    // Two sets of operand pieces in registers: while the matrix cores work on one, the other is read.  The wavefronts meet when all have
+    // read the last pieces of a tile, before they work on them: the tile's place is then free for the next but one, whose loads are issued
+    // between the last products, and the first pieces of the next arrive behind them.
     floatx16 acc[BM][BN] = {};
-    constexpr int kSteps = kLine / (int)sizeof(T);
-    const int64_t steps = (K + kSteps - 1) / kSteps;
+    uintx4 x[2][BM], y[2][BN];
+    auto read = [&](const char* tile, int s, int set) {
+#pragma unroll
+        for (int j = 0; j < BN; ++j) y[set][j] = B::piece(tile + A::kBytes, 32 * (BN * wn + j), s);
+#pragma unroll
+        for (int i = 0; i < BM; ++i) x[set][i] = A::piece(tile, 32 * (BM * wm + i), s);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto multiply_block = [&](int set, int i, int j) { acc[i][j] = multiply<T>(y[set][j], x[set][i], acc[i][j]); };
+    auto work = [&](int set) {
+#pragma unroll
+        for (int i = 0; i < BM; ++i)
+#pragma unroll
+            for (int j = 0; j < BN; ++j) multiply_block(set, i, j);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto put = [&](char* tile) {
+        a.put(tile);
+        b.put(tile + A::kBytes);
+    };
+    auto fetch_all = [&](auto full, char* tile) {  // all loads of a tile, whose places are prepared
+#pragma unroll
+        for (int f = 0; f < A::N; ++f) a.template fetch<full>(f, tile);
+#pragma unroll
+        for (int f = 0; f < B::N; ++f) b.template fetch<full>(f, tile + A::kBytes);
+        a.advance();
+        b.advance();
+    };
+    auto prepare = [&]() {
+        a.prepare();
+        b.prepare();
+    };
+    const int64_t full = K / kSteps, steps = (K + kSteps - 1) / kSteps;  // tiles that the contraction fills, and all
+    using Yes = std::true_type;
+    using No = std::false_type;
     if (steps > 0) {
-        a.fetch(tiles[0]);
-        b.fetch(tiles[0] + A::kBytes);
-        a.put(tiles[0]);
-        b.put(tiles[0] + A::kBytes);
-    }
-    for (int64_t st = 0; st < steps; ++st) {
-        const char* now = tiles[st & 1];
-        char* next = tiles[(st & 1) ^ 1];
+        prepare();
+        fetch_all(No{}, lds);
+        put(lds);
         wait_and_meet();
-        if (st + 1 < steps) {
-            a.fetch(next);
-            b.fetch(next + A::kBytes);
-        }
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            uintx4 x[BM], y[BN];
-#pragma unroll
-            for (int i = 0; i < BM; ++i) x[i] = A::piece(now, 32 * (BM * wm + i), s);
-#pragma unroll
-            for (int j = 0; j < BN; ++j) y[j] = B::piece(now + A::kBytes, 32 * (BN * wn + j), s);
-#pragma unroll
-            for (int i = 0; i < BM; ++i)
-#pragma unroll
-                for (int j = 0; j < BN; ++j) acc[i][j] = multiply<T>(y[j], x[i], acc[i][j]);
-        }
-        if (st + 1 < steps) {
-            a.put(next);
-            b.put(next + A::kBytes);
+        if (steps > 1) {
+            prepare();
+            fetch_all(No{}, lds + kBytes);
         }
     }
+    auto contract = [&](auto live) {
+        int64_t st = 0;
+        if (live && steps > 0) read(lds, 0, 0);
+        auto step = [&](auto middle) {  // middle: the next but one tile is a full one
+            char* now = lds + (st & 1) * kBytes;
+            char* next = lds + ((st & 1) ^ 1) * kBytes;
+            if constexpr (live) read(now, 1, 1);
+            if (middle || st + 2 < steps) prepare();
+            if constexpr (live) {
+                work(0);
+                read(now, 2, 0);
+                work(1);
+                read(now, 3, 1);
+                work(0);
+            }
+            if (!DIRECT && (middle || st + 1 < steps)) put(next);
+            wait_and_meet();
+            if constexpr (middle) fetch_all(Yes{}, now);
+            else if (st + 2 < steps) fetch_all(No{}, now);
+            if constexpr (live) {
+                if (middle || st + 1 < steps) read(next, 0, 0);
+                work(1);
+            }
+        };
+        for (; st + 2 < full; ++st) step(Yes{});
+        for (; st < steps; ++st) step(No{});
+    };
+    // (a wavefront whose rows lie behind the group's last has nothing to do but its share of the loads)
+    if (m0 + 32 * BM * wm < m_end) contract(Yes{});
+    else contract(No{});
 
-    const bool vec = g.vec_out != 0;
 #pragma unroll
     for (int i = 0; i < BM; ++i) {
         const int64_t r = m0 + 32 * (BM * wm + i) + (lane & 31);
         int64_t to;
+        bool none = false;  // a row of X that does not exist
         if constexpr (MODE == kWeight) to = r < m_end ? r : -1;
-        else to = row_of(g.out, r, r < m_end);
+        else {
+            to = row_of(g.out, r, r < m_end);
+            if (DIRECT && g.a.rows) none = row_of(g.a, r, r < m_end) < 0;
+        }
         if (to < 0) continue;
-        char* row = out_base + to * (MODE == kWeight ? (int64_t)g.F_out * (int64_t)sizeof(TO) : g.out.ld);
+        char* row = at.out + to * (MODE == kWeight ? (int64_t)g.F_out * (int64_t)sizeof(TO) : g.out.ld);
 #pragma unroll
         for (int j = 0; j < BN; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int c = n0 + 32 * (BN * wn + j) + 8 * q + 4 * (lane >> 5);
-                const float x[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                store4<TO>(row, c, x, N - c, vec);
+                float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                if (none) v[0] = v[1] = v[2] = v[3] = 0.f;
+                store4<TO>(row, c, v, N - c);
             }
     }
 }
 
-// grad_W[g] = the sum of its chunks' partial sums, in order (none: zeros).
+// Product and input gradient.  QUARTERS: where the tiles fill the chip's kUnits compute units some times over and then up to half of them
+// once more, those last tiles are dealt out in quarters.
+template <class T, int MODE, int WM, int WN, int BM, int BN, bool DIRECT, bool QUARTERS>
+__global__ __launch_bounds__(64 * WM * WN) void k_grouped_rows(GroupedArgs g) {
+    constexpr int TM = 32 * WM * BM, TN = 32 * WN * BN;
+    __shared__ __attribute__((aligned(128))) char lds[2 * (TM + TN) * kLine];
+    const int N = MODE == kInput ? g.F_in : g.F_out;
+    const int nt = (N + TN - 1) / TN;
+    int64_t tiles;
+    find_group(g.offsets, g.G, g.m, TM, -1, &tiles);
+    tiles *= nt;
+    // Workgroups b, b + 8, .. run on one XCD: it gets neighbouring tiles, which share rows and weights in its L2.
+    int64_t whole = tiles, b = blockIdx.x;
+    if (QUARTERS && tiles % kUnits <= kUnits / 2) whole = tiles / kUnits * kUnits;
+    int quarter = -1;
+    const bool last = b >= (whole + 7) / 8 * 8;
+    if (last) b -= (whole + 7) / 8 * 8;
+    const int64_t count = last ? 4 * (tiles - whole) : whole, per = (count + 7) / 8;
+    int64_t mine = (b & 7) * per + (b >> 3);
+    if ((b >> 3) >= per || mine >= count) return;
+    if (last) {
+        quarter = (int)(mine & 3);
+        mine = whole + (mine >> 2);
+    }
+    int64_t unused;
+    const Span s = find_group(g.offsets, g.G, g.m, TM, mine / nt, &unused);
+    Place at = {s.g, uniform(s.first + (mine / nt - s.chunk0) * TM), uniform(s.last), __builtin_amdgcn_readfirstlane((int)(mine % nt) * TN), 0, 0, const_cast<char*>(g.out.data)};
+    if (!QUARTERS || quarter < 0) {
+        form_tile<T, T, MODE, WM, WN, BM, BN, DIRECT, false>(g, at, lds);
+    } else if constexpr (QUARTERS) {
+        at.m0 += (quarter & 1) * (TM / 2);
+        at.n0 += (quarter >> 1) * (TN / 2);
+        if (at.m0 < at.m_end && at.n0 < N) form_tile<T, T, MODE, WM, WN, BM / 2, BN / 2, DIRECT, false>(g, at, lds);
+    }
+}
+
+template <class T, class TO, int WM, int WN, int BM, int BN, bool DIRECT, bool LIST>
+__global__ __launch_bounds__(64 * WM * WN) void k_grouped_weight(GroupedArgs g) {
+    constexpr int TM = 32 * WM * BM, TN = 32 * WN * BN;
+    __shared__ __attribute__((aligned(128))) char lds[2 * (TM + TN) * kLine + (DIRECT && LIST ? 2048 : 0)];
+    const int mt = (g.F_in + TM - 1) / TM, nt = (g.F_out + TN - 1) / TN;
+    // (the tiles of one group or chunk are dealt to all XCDs: groups differ in size)
+    const int per_group = mt * nt, in = (int)(blockIdx.x % per_group), share = per_group / 8;
+    const int64_t chunk = blockIdx.x / per_group;
+    const int tile = per_group % 8 == 0 ? (in & 7) * share + (in >> 3) : in;
+    Place at = {0, (int64_t)(tile / nt) * TM, g.F_in, (tile % nt) * TN, 0, 0, const_cast<char*>(g.out.data)};
+    if (g.per) {
+        int64_t total;
+        const Span s = find_group(g.offsets, g.G, g.m, g.per, chunk, &total);
+        if (s.g < 0) return;
+        at.first = uniform(s.first + (chunk - s.chunk0) * g.per);
+        at.last = uniform(min(at.first + g.per, s.last));
+        at.out = reinterpret_cast<char*>(g.part + chunk * g.F_in * g.F_out);
+    } else {
+        at.first = min(max((int64_t)g.offsets[chunk], (int64_t)0), g.m);
+        at.last = max(at.first, min((int64_t)g.offsets[chunk + 1], g.m));
+        at.out += chunk * g.F_in * g.F_out * (int64_t)sizeof(TO);
+    }
+    form_tile<T, TO, kWeight, WM, WN, BM, BN, DIRECT, LIST>(g, at, lds);
+}
+
+// grad_W[g] = the sum of its chunks' partial sums, in order (none: zeros).  Four elements to a thread.
 template <class TO>
 __global__ __launch_bounds__(256) void k_grouped_sum(GroupedArgs g, TO* __restrict__ grad_W) {
     const int64_t size = (int64_t)g.F_in * g.F_out;
@@ -456,21 +615,37 @@ __global__ __launch_bounds__(256) void k_grouped_sum(GroupedArgs g, TO* __restri
         }
     }
     __syncthreads();
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (e >= size) return;
+    typedef float any_floatx4 __attribute__((ext_vector_type(4), aligned(4)));
     const float* p = g.part + span[0] * size + e;
     const int64_t count = span[1];
-    float sum = 0.f;
-    int64_t c = 0;
-    for (; c + 8 <= count; c += 8) {
-        float x[8];
+    const int valid = (int)min(size - e, (int64_t)4);
+    float sum[4] = {};
+    if (valid == 4) {
+        int64_t c = 0;
+        for (; c + 4 <= count; c += 4) {
+            floatx4 x[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = p[(c + i) * size];
+            for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const any_floatx4*>(p + (c + i) * size);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += x[i];
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) sum[q] += x[i][q];
+        }
+        for (; c < count; ++c) {
+            const floatx4 x = *reinterpret_cast<const any_floatx4*>(p + c * size);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum[q] += x[q];
+        }
+    } else {
+        for (int64_t c = 0; c < count; ++c)
+#pragma unroll
+            for (int q = 0; q < 3; ++q)
+                if (q < valid) sum[q] += p[c * size + q];
     }
-    for (; c < count; ++c) sum += p[c * size];
-    grad_W[blockIdx.y * size + e] = Num<TO>::from(sum);
+    TO* to = grad_W + blockIdx.y * size + e;
+    store4<TO>(reinterpret_cast<char*>(to), 0, sum, valid);
 }
 
 // ---------------------------------------------------------------- host side
@@ -527,20 +702,32 @@ Side side(const epp_rows_t& x, int size) { return {static_cast<const char*>(x.da
 // Tiles of `tile` entries that m entries in G groups can make.
 int64_t most_tiles(int64_t m, int64_t G, int64_t tile) { return (m + std::min(G, m) * (tile - 1)) / tile; }
 
-template <class T, class TO, int MODE, int WM, int WN, int BM, int BN>
-int launch(const GroupedArgs& g, int64_t blocks, bool direct, hipStream_t s) {
-    if (blocks > 0x7FFFFFFF) { epp_set_error("%lld workgroups in one launch", (long long)blocks); return EPP_ERR_TOO_LARGE; }
-    if (direct) hipLaunchKernelGGL((k_grouped<T, TO, MODE, WM, WN, BM, BN, true>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, g);
-    else hipLaunchKernelGGL((k_grouped<T, TO, MODE, WM, WN, BM, BN, false>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, g);
+int too_many(int64_t blocks) { epp_set_error("%lld workgroups in one launch", (long long)blocks); return EPP_ERR_TOO_LARGE; }
+
+template <class T, int MODE, int WM, int WN, int BM, int BN, bool DIRECT, bool QUARTERS>
+int launch_rows_of(const GroupedArgs& g, hipStream_t s) {
+    constexpr int TM = 32 * WM * BM, TN = 32 * WN * BN;
+    const int N = MODE == kInput ? g.F_in : g.F_out;
+    int64_t blocks = most_tiles(g.m, g.G, TM) * ((N + TN - 1) / TN) + 16;
+    if (QUARTERS) blocks += 3 * (kUnits / 2);
+    if (blocks > 0x7FFFFFFF) return too_many(blocks);
+    hipLaunchKernelGGL((k_grouped_rows<T, MODE, WM, WN, BM, BN, DIRECT, QUARTERS>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, g);
     EPP_HIP_TRY(hipGetLastError());
     return EPP_OK;
 }
 
+// 16 bits: tiles of 256 x 256, which fetch half as much a product as tiles of 128 x 128 but come one to a compute unit, where there are enough
+// of them and the width does not waste a part of each.  bfloat16, groups of exponentially distributed sizes, 128 / 256 wide, us: 2,048 entries,
+// 16 groups, 4,096 x 4,096 (about 256 tiles of 256) 173 / 154; 32,768, 32, 4,096 x 2,048 663 / 593; 32,768, 64, 2,048 x 512 (320) 112 / 101;
+// but 8,192, 64, 2,048 x 512 (128) 34 / 55, 512, 4, 4,096 x 4,096 (64) 49 / 85, and 32,768, 4, 256 x 384 (a quarter wasted) 24 / 29.
+bool large_tiles(int64_t rows, int width) { return (width % 256 == 0 || width >= 1024) && rows * ((width + 255) / 256) >= 192; }
+
 template <class T, int MODE>
 int launch_rows(const GroupedArgs& g, bool direct, hipStream_t s) {
-    const int N = MODE == kInput ? g.F_in : g.F_out;
-    const int64_t blocks = (most_tiles(g.m, g.G, 128) * ((N + 127) / 128) + 7) / 8 * 8;
-    return launch<T, T, MODE, 2, 2, 2, 2>(g, blocks, direct, s);
+    if constexpr (sizeof(T) == 2)
+        if (direct && large_tiles(g.m / 256 + g.G / 2, MODE == kInput ? g.F_in : g.F_out)) return launch_rows_of<T, MODE, 2, 4, 4, 2, true, true>(g, s);
+    if (direct) return launch_rows_of<T, MODE, 2, 2, 2, 2, true, false>(g, s);
+    return launch_rows_of<T, MODE, 2, 2, 2, 2, false, false>(g, s);
 }
 
 // product (X, W -> out) and input gradient (grad_out, W -> grad_X)
@@ -566,8 +753,9 @@ int grouped_rows(int mode, int type, const epp_rows_t* in, const void* W, const 
     g.G = G;
     g.F_in = F_in;
     g.F_out = F_out;
-    g.vec_out = (reinterpret_cast<uintptr_t>(out->data) | (uintptr_t)g.out.ld) % (4 * (unsigned)size) == 0;
-    const bool direct = aligned(g.a, w_in * size) && reinterpret_cast<uintptr_t>(W) % 16 == 0 && (F_out * size) % 16 == 0;
+    // (with a list of rows, direct loads find them by 32 bits; and there has to be one)
+    const bool direct = aligned(g.a, w_in * size) && reinterpret_cast<uintptr_t>(W) % 16 == 0 && (F_out * size) % 16 == 0 && in->n > 0 && g.a.ld < (1 << 24) &&
+                        (!in->rows || g.a.n * g.a.ld < (1ll << 32));
     if (mode == kInput) {
         if (type == EPP_FLOAT32) return launch_rows<float, kInput>(g, direct, s);
         if (type == EPP_BFLOAT16) return launch_rows<__bf16, kInput>(g, direct, s);
@@ -582,25 +770,44 @@ int grouped_rows(int mode, int type, const epp_rows_t* in, const void* W, const 
 struct Chunks { int64_t per, count; };
 Chunks chunking(int64_t m, int G, int F_in, int F_out) {
     const int64_t tiles = (int64_t)((F_in + 127) / 128) * ((F_out + 127) / 128);
-    // (one group may hold nearly all entries: its tiles alone have to fill the chip)
-    const int64_t wanted = 512 / tiles;
-    if (wanted <= 1 || m < 512) return {0, G};
-    const int64_t per = std::max<int64_t>((m + wanted - 1) / wanted, 256);
+    // (groups differ in size: half of them have to fill the chip; chunks of fewer than 512 entries take less time than their partial sums)
+    const int64_t at_once = tiles * ((G + 1) / 2), wanted = (512 + at_once - 1) / at_once;
+    if (wanted <= 1 || m < 512 * (int64_t)G) return {0, G};
+    const int64_t per = std::max<int64_t>((m * 2 / G + wanted - 1) / wanted, 512);
     return {per, most_tiles(m, G, per)};
+}
+
+template <class T, class TO, int WM, int WN, int BM, int BN, bool DIRECT, bool LIST>
+int launch_weight_of(const GroupedArgs& g, int64_t chunks, hipStream_t s) {
+    constexpr int TM = 32 * WM * BM, TN = 32 * WN * BN;
+    const int64_t blocks = chunks * ((g.F_in + TM - 1) / TM) * ((g.F_out + TN - 1) / TN);
+    if (blocks > 0x7FFFFFFF) return too_many(blocks);
+    hipLaunchKernelGGL((k_grouped_weight<T, TO, WM, WN, BM, BN, DIRECT, LIST>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, g);
+    EPP_HIP_TRY(hipGetLastError());
+    return EPP_OK;
+}
+
+template <class T, class TO>
+int launch_weight_tiles(const GroupedArgs& g, int64_t chunks, bool direct, hipStream_t s) {
+    if constexpr (sizeof(T) == 2)
+        if (direct && !g.per && g.F_in >= 256 && large_tiles((int64_t)g.G * ((g.F_in + 255) / 256) / 3, g.F_out)) {
+            if (g.a.rows || g.b.rows) return launch_weight_of<T, TO, 2, 4, 4, 2, true, true>(g, chunks, s);
+            return launch_weight_of<T, TO, 2, 4, 4, 2, true, false>(g, chunks, s);
+        }
+    if (direct && (g.a.rows || g.b.rows)) return launch_weight_of<T, TO, 2, 2, 2, 2, true, true>(g, chunks, s);
+    if (direct) return launch_weight_of<T, TO, 2, 2, 2, 2, true, false>(g, chunks, s);
+    return launch_weight_of<T, TO, 2, 2, 2, 2, false, true>(g, chunks, s);
 }
 
 template <class T, class TO>
 int launch_weight(GroupedArgs g, const Chunks& c, bool direct, TO* grad_W, hipStream_t s) {
-    const int64_t tiles = (int64_t)((g.F_in + 127) / 128) * ((g.F_out + 127) / 128);
     if (!c.per) {
         g.out.data = reinterpret_cast<const char*>(grad_W);
-        g.vec_out = g.F_out % 4 == 0 && reinterpret_cast<uintptr_t>(grad_W) % (4 * sizeof(TO)) == 0;
-        return launch<T, TO, kWeight, 2, 2, 2, 2>(g, c.count * tiles, direct, s);
+        return launch_weight_tiles<T, TO>(g, c.count, direct, s);
     }
-    g.vec_out = g.F_out % 4 == 0;
-    EPP_TRY((launch<T, float, kWeight, 2, 2, 2, 2>(g, c.count * tiles, direct, s)));
+    EPP_TRY((launch_weight_tiles<T, float>(g, c.count, direct, s)));
     const int64_t size = (int64_t)g.F_in * g.F_out;
-    hipLaunchKernelGGL((k_grouped_sum<TO>), dim3((unsigned)((size + 255) / 256), (unsigned)g.G), dim3(256), 0, s, g, grad_W);
+    hipLaunchKernelGGL((k_grouped_sum<TO>), dim3((unsigned)((size + 1023) / 1024), (unsigned)g.G), dim3(256), 0, s, g, grad_W);
     EPP_HIP_TRY(hipGetLastError());
     return EPP_OK;
 }
@@ -657,7 +864,7 @@ extern "C" int epp_grouped_weight_gradient(int type, const epp_rows_t* X, const 
     const Chunks c = chunking(m, G, F_in, F_out);
     g.per = c.per;
     g.part = static_cast<float*>(workspace);
-    const bool direct = aligned(g.a, F_in * size) && aligned(g.b, F_out * size);
+    const bool direct = aligned(g.a, F_in * size) && aligned(g.b, F_out * size) && std::max(g.a.ld, g.b.ld) < (1 << 26);
     hipStream_t s = (hipStream_t)stream;
     if (type == EPP_FLOAT32) return launch_weight<float, float>(g, c, direct, static_cast<float*>(grad_W), s);
     if (type == EPP_BFLOAT16) {
