@@ -1,0 +1,115 @@
+// What the grouped products' kernels share (csrc/epp_grouped.hip, csrc/epp_grouped_narrow.hip, csrc/epp_grouped_few.hip).
+#pragma once
+
+#include "epp_internal.h"
+
+namespace epp_grouped {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef unsigned int uintx4 __attribute__((ext_vector_type(4)));
+typedef unsigned int uintx2 __attribute__((ext_vector_type(2)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef short shortx8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bfloatx8 __attribute__((ext_vector_type(8)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+
+constexpr int kUnits = 256;  // compute units
+
+enum Mode { kProduct, kInput, kWeight };
+
+struct Side {           // a matrix and the rows of it that entries name
+    const char* data;
+    int64_t n, ld;      // rows, bytes from row to row
+    const int32_t* rows;
+};
+struct GroupedArgs {
+    Side a, b;          // product, input gradient: a, weight gradient: both
+    Side out;
+    const char* W;
+    const int32_t* offsets;
+    int64_t m;
+    int G, F_in, F_out;
+    int64_t per;        // weight gradient: entries to a chunk (0: whole groups)
+    float* part;        // .. and its partial sums
+};
+
+// ---------------------------------------------------------------- numbers
+template <class T> struct Num;
+template <> struct Num<float> {
+    static __device__ __forceinline__ float from(float x) { return x; }
+};
+template <> struct Num<__bf16> {
+    static __device__ __forceinline__ __bf16 from(float x) { return (__bf16)x; }
+};
+template <> struct Num<_Float16> {
+    static __device__ __forceinline__ _Float16 from(float x) { return (_Float16)x; }
+};
+
+// The same value in all lanes, and the compiler told so.
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+    return (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)x) | (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32);
+}
+__device__ __forceinline__ const char* uniform(const char* p) { return reinterpret_cast<const char*>(uniform(reinterpret_cast<int64_t>(p))); }
+
+struct Span { int g; int64_t first, last, chunk0; };  // a group (-1: none), its entries, its first tile
+
+// The group that holds the `tile`-th of the tiles of `per` entries, and how many tiles there are.  Offsets are kept inside
+// [0, m]; a group that would end before it begins is empty.
+__device__ __forceinline__ Span find_group(const int32_t* __restrict__ offsets, int G, int64_t m, int64_t per, int64_t tile, int64_t* total) {
+    const int lane = threadIdx.x & 63;
+    Span found = {-1, 0, 0, 0};
+    int64_t before = 0;
+    for (int g0 = 0; g0 < G; g0 += 64) {
+        const int g = g0 + lane;
+        int64_t lo = 0, hi = 0;
+        if (g < G) {
+            lo = min(max((int64_t)offsets[g], (int64_t)0), m);
+            hi = min(max((int64_t)offsets[g + 1], (int64_t)0), m);
+        }
+        const int tiles = hi > lo ? (int)((uint32_t)(hi - lo + per - 1) / (uint32_t)per) : 0;
+        int upto = tiles;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int x = __shfl_up(upto, d, 64);
+            if (lane >= d) upto += x;
+        }
+        const unsigned long long past = __ballot(before + upto > tile);
+        if (found.g < 0 && past) {
+            const int l = __ffsll((long long)past) - 1;
+            found = {g0 + l, __shfl(lo, l, 64), __shfl(hi, l, 64), before + __shfl(upto - tiles, l, 64)};
+        }
+        before += __shfl(upto, 63, 64);
+    }
+    *total = uniform(before);
+    found.g = __builtin_amdgcn_readfirstlane(found.g);
+    return found;
+}
+
+__device__ __forceinline__ int64_t row_of(const Side& s, int64_t i, bool valid) {  // -1: no such row
+    if (!valid) return -1;
+    const int64_t r = s.rows ? (int64_t)s.rows[i] : i;
+    return r >= 0 && r < s.n ? r : -1;
+}
+// Four neighbouring results of a row; `valid` of them exist.  (A store needs no alignment beyond the element's.)
+template <class T>
+__device__ __forceinline__ void store4(char* row, int col, const float (&x)[4], int valid) {
+    T* p = reinterpret_cast<T*>(row) + col;
+    if (valid >= 4) {
+        typedef T vec4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+        *reinterpret_cast<vec4*>(p) = vec4{Num<T>::from(x[0]), Num<T>::from(x[1]), Num<T>::from(x[2]), Num<T>::from(x[3])};
+    } else {
+#pragma unroll
+        for (int c = 0; c < 3; ++c)
+            if (c < valid) p[c] = Num<T>::from(x[c]);
+    }
+}
+
+// Kernels of their own for narrow fp32 matrices (csrc/epp_grouped_narrow.hip).
+bool narrow_rows(int K, int N);     // of contraction K onto N columns
+int launch_narrow_rows(bool input, const GroupedArgs& g, hipStream_t s);
+bool narrow_weight(int F_in, int F_out);
+int64_t narrow_weight_chunk(int64_t m);  // entries to a chunk of partial sums
+int launch_narrow_weight(const GroupedArgs& g, int64_t chunks, hipStream_t s);
+
+}  // namespace epp_grouped

@@ -25,56 +25,18 @@
 // the result's column, so that a lane holds four neighbouring columns of one row.
 // Sums are fp32; 16-bit results are rounded once, when they are written.
 
-#include "epp_internal.h"
+#include "epp_grouped.h"
+
+using namespace epp_grouped;
 
 namespace {
-
-typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef unsigned int uintx4 __attribute__((ext_vector_type(4)));
-typedef unsigned int uintx2 __attribute__((ext_vector_type(2)));
-typedef short shortx4 __attribute__((ext_vector_type(4)));
-typedef short shortx8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bfloatx8 __attribute__((ext_vector_type(8)));
-typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 
 constexpr int kMaxGroups = 2048;
 constexpr int kMaxWidth = 1 << 16;
 constexpr int kLine = 128;   // bytes of the contraction in a tile
-constexpr int kUnits = 256;  // compute units
-
-enum Mode { kProduct, kInput, kWeight };
 
 __device__ __attribute__((aligned(128))) unsigned int g_zeros[32] = {};
 __device__ int32_t g_none = -1;  // no row
-
-struct Side {           // a matrix and the rows of it that entries name
-    const char* data;
-    int64_t n, ld;      // rows, bytes from row to row
-    const int32_t* rows;
-};
-struct GroupedArgs {
-    Side a, b;          // product, input gradient: a, weight gradient: both
-    Side out;
-    const char* W;
-    const int32_t* offsets;
-    int64_t m;
-    int G, F_in, F_out;
-    int64_t per;        // weight gradient: entries to a chunk (0: whole groups)
-    float* part;        // .. and its partial sums
-};
-
-// ---------------------------------------------------------------- numbers
-template <class T> struct Num;
-template <> struct Num<float> {
-    static __device__ __forceinline__ float from(float x) { return x; }
-};
-template <> struct Num<__bf16> {
-    static __device__ __forceinline__ __bf16 from(float x) { return (__bf16)x; }
-};
-template <> struct Num<_Float16> {
-    static __device__ __forceinline__ _Float16 from(float x) { return (_Float16)x; }
-};
 
 // One piece (16 bytes) of the contraction of both operands.
 template <class T>
@@ -89,47 +51,6 @@ __device__ __forceinline__ floatx16 multiply(uintx4 a, uintx4 b, floatx16 c) {
     } else {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, a), __builtin_bit_cast(halfx8, b), c, 0, 0, 0);
     }
-}
-
-// The same value in all lanes, and the compiler told so.
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-    return (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)x) | (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32);
-}
-__device__ __forceinline__ const char* uniform(const char* p) { return reinterpret_cast<const char*>(uniform(reinterpret_cast<int64_t>(p))); }
-
-// ---------------------------------------------------------------- groups
-struct Span { int g; int64_t first, last, chunk0; };  // a group (-1: none), its entries, its first tile
-
-// The group that holds the `tile`-th of the tiles of `per` entries, and how many tiles there are.  Offsets are kept inside
-// [0, m]; a group that would end before it begins is empty.
-__device__ __forceinline__ Span find_group(const int32_t* __restrict__ offsets, int G, int64_t m, int64_t per, int64_t tile, int64_t* total) {
-    const int lane = threadIdx.x & 63;
-    Span found = {-1, 0, 0, 0};
-    int64_t before = 0;
-    for (int g0 = 0; g0 < G; g0 += 64) {
-        const int g = g0 + lane;
-        int64_t lo = 0, hi = 0;
-        if (g < G) {
-            lo = min(max((int64_t)offsets[g], (int64_t)0), m);
-            hi = min(max((int64_t)offsets[g + 1], (int64_t)0), m);
-        }
-        const int tiles = hi > lo ? (int)((hi - lo + per - 1) / per) : 0;
-        int upto = tiles;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int x = __shfl_up(upto, d, 64);
-            if (lane >= d) upto += x;
-        }
-        const unsigned long long past = __ballot(before + upto > tile);
-        if (found.g < 0 && past) {
-            const int l = __ffsll((long long)past) - 1;
-            found = {g0 + l, __shfl(lo, l, 64), __shfl(hi, l, 64), before + __shfl(upto - tiles, l, 64)};
-        }
-        before += __shfl(upto, 63, 64);
-    }
-    *total = uniform(before);
-    found.g = __builtin_amdgcn_readfirstlane(found.g);
-    return found;
 }
 
 // ---------------------------------------------------------------- operand tiles
@@ -150,11 +71,6 @@ __device__ __forceinline__ void load_to_lds(const char* base, unsigned off, unsi
 // All loads of this wavefront have arrived and all its LDS reads are done; then the same for the workgroup's.
 __device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-__device__ __forceinline__ int64_t row_of(const Side& s, int64_t i, bool valid) {  // -1: no such row
-    if (!valid) return -1;
-    const int64_t r = s.rows ? (int64_t)s.rows[i] : i;
-    return r >= 0 && r < s.n ? r : -1;
-}
 __device__ __forceinline__ const char* zeros() { return reinterpret_cast<const char*>(g_zeros); }
 // A piece with `valid` elements (0 .. a piece's), through registers.
 template <class T>
@@ -366,20 +282,6 @@ struct LinesOfWidth {
     }
 };
 
-// Four neighbouring results of a row; `valid` of them exist.  (A store needs no alignment beyond the element's.)
-template <class T>
-__device__ __forceinline__ void store4(char* row, int col, const float (&x)[4], int valid) {
-    T* p = reinterpret_cast<T*>(row) + col;
-    if (valid >= 4) {
-        typedef T vec4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-        *reinterpret_cast<vec4*>(p) = vec4{Num<T>::from(x[0]), Num<T>::from(x[1]), Num<T>::from(x[2]), Num<T>::from(x[3])};
-    } else {
-#pragma unroll
-        for (int c = 0; c < 3; ++c)
-            if (c < valid) p[c] = Num<T>::from(x[c]);
-    }
-}
-
 // Where a tile of the result is.
 struct Place {
     int g;                  // group (product, input gradient)
@@ -586,11 +488,14 @@ __global__ __launch_bounds__(64 * WM * WN) void k_grouped_weight(GroupedArgs g) 
     form_tile<T, TO, kWeight, WM, WN, BM, BN, DIRECT, LIST>(g, at, lds);
 }
 
-// grad_W[g] = the sum of its chunks' partial sums, in order (none: zeros).  Four elements to a thread.
-template <class TO>
+// grad_W[g] = the sum of its chunks' partial sums, in order (none: zeros).  Four elements to a thread; SLICES threads share the chunks of
+// them, every one a run of consecutive chunks.
+template <class TO, int SLICES>
 __global__ __launch_bounds__(256) void k_grouped_sum(GroupedArgs g, TO* __restrict__ grad_W) {
+    constexpr int kThreads = 256 / SLICES;  // that share no element
     const int64_t size = (int64_t)g.F_in * g.F_out;
     __shared__ int64_t span[2];
+    __shared__ float part[SLICES > 1 ? SLICES : 1][kThreads][4];
     if (threadIdx.x < 64) {
         const int lane = threadIdx.x;
         int64_t before = 0, count = 0;
@@ -599,7 +504,7 @@ __global__ __launch_bounds__(256) void k_grouped_sum(GroupedArgs g, TO* __restri
             int64_t tiles = 0;
             if (h <= (int)blockIdx.y) {
                 const int64_t lo = min(max((int64_t)g.offsets[h], (int64_t)0), g.m), hi = min(max((int64_t)g.offsets[h + 1], (int64_t)0), g.m);
-                tiles = hi > lo ? (hi - lo + g.per - 1) / g.per : 0;
+                tiles = hi > lo ? (uint32_t)(hi - lo + g.per - 1) / (uint32_t)g.per : 0;
             }
             if (h == (int)blockIdx.y) count = tiles;
             else before += tiles;
@@ -615,16 +520,16 @@ __global__ __launch_bounds__(256) void k_grouped_sum(GroupedArgs g, TO* __restri
         }
     }
     __syncthreads();
-    const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (e >= size) return;
+    const int slice = threadIdx.x / kThreads, lane = threadIdx.x % kThreads;
+    const int64_t e = ((int64_t)blockIdx.x * kThreads + lane) * 4;
+    const int64_t share = (span[1] + SLICES - 1) / SLICES, first = min(slice * share, span[1]), last = min(first + share, span[1]);
     typedef float any_floatx4 __attribute__((ext_vector_type(4), aligned(4)));
     const float* p = g.part + span[0] * size + e;
-    const int64_t count = span[1];
-    const int valid = (int)min(size - e, (int64_t)4);
+    const int valid = (int)max(min(size - e, (int64_t)4), (int64_t)0);
     float sum[4] = {};
     if (valid == 4) {
-        int64_t c = 0;
-        for (; c + 4 <= count; c += 4) {
+        int64_t c = first;
+        for (; c + 4 <= last; c += 4) {
             floatx4 x[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const any_floatx4*>(p + (c + i) * size);
@@ -633,19 +538,28 @@ __global__ __launch_bounds__(256) void k_grouped_sum(GroupedArgs g, TO* __restri
 #pragma unroll
                 for (int q = 0; q < 4; ++q) sum[q] += x[i][q];
         }
-        for (; c < count; ++c) {
+        for (; c < last; ++c) {
             const floatx4 x = *reinterpret_cast<const any_floatx4*>(p + c * size);
 #pragma unroll
             for (int q = 0; q < 4; ++q) sum[q] += x[q];
         }
     } else {
-        for (int64_t c = 0; c < count; ++c)
+        for (int64_t c = first; c < last; ++c)
 #pragma unroll
             for (int q = 0; q < 3; ++q)
                 if (q < valid) sum[q] += p[c * size + q];
     }
-    TO* to = grad_W + blockIdx.y * size + e;
-    store4<TO>(reinterpret_cast<char*>(to), 0, sum, valid);
+    if constexpr (SLICES > 1) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) part[slice][lane][q] = sum[q];
+        __syncthreads();
+        if (slice) return;
+#pragma unroll
+        for (int x = 1; x < SLICES; ++x)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum[q] += part[x][lane][q];
+    }
+    if (valid) store4<TO>(reinterpret_cast<char*>(grad_W + blockIdx.y * size + e), 0, sum, valid);
 }
 
 // ---------------------------------------------------------------- host side
@@ -724,6 +638,8 @@ bool large_tiles(int64_t rows, int width) { return (width % 256 == 0 || width >=
 
 template <class T, int MODE>
 int launch_rows(const GroupedArgs& g, bool direct, hipStream_t s) {
+    if constexpr (sizeof(T) == 4)
+        if (narrow_rows(MODE == kInput ? g.F_out : g.F_in, MODE == kInput ? g.F_in : g.F_out)) return launch_narrow_rows(MODE == kInput, g, s);
     if constexpr (sizeof(T) == 2)
         if (direct && large_tiles(g.m / 256 + g.G / 2, MODE == kInput ? g.F_in : g.F_out)) return launch_rows_of<T, MODE, 2, 4, 4, 2, true, true>(g, s);
     if (direct) return launch_rows_of<T, MODE, 2, 2, 2, 2, true, false>(g, s);
@@ -768,7 +684,11 @@ int grouped_rows(int mode, int type, const epp_rows_t* in, const void* W, const 
 
 // How the weight gradient cuts its entries: chunks of `per` entries of a group, at most `count` of them; per = 0: whole groups.
 struct Chunks { int64_t per, count; };
-Chunks chunking(int64_t m, int G, int F_in, int F_out) {
+Chunks chunking(bool fp32, int64_t m, int G, int F_in, int F_out) {
+    if (fp32 && narrow_weight(F_in, F_out)) {
+        const int64_t per = narrow_weight_chunk(m);
+        return {per, std::max<int64_t>(most_tiles(m, G, per), 1)};
+    }
     const int64_t tiles = (int64_t)((F_in + 127) / 128) * ((F_out + 127) / 128);
     // (groups differ in size: half of them have to fill the chip; chunks of fewer than 512 entries take less time than their partial sums)
     const int64_t at_once = tiles * ((G + 1) / 2), wanted = (512 + at_once - 1) / at_once;
@@ -799,17 +719,29 @@ int launch_weight_tiles(const GroupedArgs& g, int64_t chunks, bool direct, hipSt
     return launch_weight_of<T, TO, 2, 2, 2, 2, false, true>(g, chunks, s);
 }
 
+template <class TO>
+int launch_sum(const GroupedArgs& g, int64_t chunks, TO* grad_W, hipStream_t s) {
+    // (many chunks of small matrices: 16 threads to an element)
+    const int64_t quads = ((int64_t)g.F_in * g.F_out + 3) / 4;
+    if (chunks >= 16 * (int64_t)g.G) hipLaunchKernelGGL((k_grouped_sum<TO, 16>), dim3((unsigned)((quads + 15) / 16), (unsigned)g.G), dim3(256), 0, s, g, grad_W);
+    else hipLaunchKernelGGL((k_grouped_sum<TO, 1>), dim3((unsigned)((quads + 255) / 256), (unsigned)g.G), dim3(256), 0, s, g, grad_W);
+    EPP_HIP_TRY(hipGetLastError());
+    return EPP_OK;
+}
+
 template <class T, class TO>
 int launch_weight(GroupedArgs g, const Chunks& c, bool direct, TO* grad_W, hipStream_t s) {
+    if constexpr (sizeof(T) == 4)
+        if (narrow_weight(g.F_in, g.F_out)) {
+            EPP_TRY(launch_narrow_weight(g, c.count, s));
+            return launch_sum<TO>(g, c.count, grad_W, s);
+        }
     if (!c.per) {
         g.out.data = reinterpret_cast<const char*>(grad_W);
         return launch_weight_tiles<T, TO>(g, c.count, direct, s);
     }
     EPP_TRY((launch_weight_tiles<T, float>(g, c.count, direct, s)));
-    const int64_t size = (int64_t)g.F_in * g.F_out;
-    hipLaunchKernelGGL((k_grouped_sum<TO>), dim3((unsigned)((size + 1023) / 1024), (unsigned)g.G), dim3(256), 0, s, g, grad_W);
-    EPP_HIP_TRY(hipGetLastError());
-    return EPP_OK;
+    return launch_sum<TO>(g, c.count, grad_W, s);
 }
 
 }  // namespace
@@ -826,8 +758,12 @@ extern "C" int epp_grouped_input_gradient(int type, const epp_rows_t* grad_out, 
 
 extern "C" int64_t epp_grouped_weight_gradient_workspace(int64_t m, int G, int F_in, int F_out) {
     EPP_TRY(check_groups(m, G, F_in, F_out));
-    const Chunks c = chunking(m, G, F_in, F_out);
-    return c.per ? c.count * F_in * F_out * (int64_t)sizeof(float) : 16;
+    int64_t bytes = 16;  // (for operands of any type)
+    for (const bool fp32 : {false, true}) {
+        const Chunks c = chunking(fp32, m, G, F_in, F_out);
+        if (c.per) bytes = std::max<int64_t>(bytes, c.count * F_in * F_out * (int64_t)sizeof(float));
+    }
+    return bytes;
 }
 
 extern "C" int epp_grouped_weight_gradient(int type, const epp_rows_t* X, const epp_rows_t* grad_out, const int32_t* offsets, int G,
@@ -861,7 +797,7 @@ extern "C" int epp_grouped_weight_gradient(int type, const epp_rows_t* X, const 
     g.G = G;
     g.F_in = F_in;
     g.F_out = F_out;
-    const Chunks c = chunking(m, G, F_in, F_out);
+    const Chunks c = chunking(type == EPP_FLOAT32, m, G, F_in, F_out);
     g.per = c.per;
     g.part = static_cast<float*>(workspace);
     const bool direct = aligned(g.a, F_in * size) && aligned(g.b, F_out * size) && std::max(g.a.ld, g.b.ld) < (1 << 26);

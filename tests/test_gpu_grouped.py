@@ -117,6 +117,22 @@ def test_few_rows(m, G, Fi, Fo, dtype):
     run_rows(sizes, Fi, Fo, dtype, True, 12)
 
 
+@pytest.mark.parametrize("Fi", [1, 4, 30, 32, 33, 40, 64, 72, 95, 96, 97, 128])
+@pytest.mark.parametrize("Fo", [2, 16, 32, 35, 56, 64, 66, 96, 100, 128])
+def test_narrow_floats(Fi, Fo):
+    """Widths of up to 128, at the edges of the blocks of 32 and of the pieces of 16 bytes; few entries and many."""
+    for sizes in ([70, 0, 50, 1], [9_000, 31, 8_001, 700]):
+        run_rows(sizes, Fi, Fo, torch.float32, False, Fi)
+        run_rows(sizes, Fi, Fo, torch.float32, True, Fo)
+        m, offsets = sum(sizes), offsets_of(sizes)
+        x, d = randn(m, Fi, seed=13), randn(m, Fo, seed=14)
+        ws = torch.empty(epp.epp_grouped_weight_gradient_workspace(m, 4, Fi, Fo), dtype=torch.uint8, device=dev())
+        got = torch.empty(4, Fi, Fo, device=dev())
+        epp.epp_grouped_weight_gradient(x, d, offsets, got, ws)
+        want, size, terms = weight_gradient(x, d, offsets, m)
+        assert_sums(got, want, size, terms + 520)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_many_rows(dtype):
     sizes = [3000, 0, 1111, 5000]
