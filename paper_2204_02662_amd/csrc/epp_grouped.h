@@ -91,6 +91,18 @@ __device__ __forceinline__ int64_t row_of(const Side& s, int64_t i, bool valid) 
     const int64_t r = s.rows ? (int64_t)s.rows[i] : i;
     return r >= 0 && r < s.n ? r : -1;
 }
+__device__ __forceinline__ unsigned lds_address(const void* p) {
+    return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+// 16 bytes a lane into LDS, lane after lane from `to` on.  Complete once vmcnt says so (wait_and_meet).  (Not the compiler's builtin: it waits
+// for all of these loads before every transposing LDS read, those of the next tile included.  The compiler writes m0 right before its own uses.)
+__device__ __forceinline__ void load_to_lds(const char* from, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+__device__ __forceinline__ void load_to_lds(const char* base, unsigned off, unsigned to) {  // (base the same in all lanes)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+}
+
 // Four neighbouring results of a row; `valid` of them exist.  (A store needs no alignment beyond the element's.)
 template <class T>
 __device__ __forceinline__ void store4(char* row, int col, const float (&x)[4], int valid) {
@@ -104,6 +116,10 @@ __device__ __forceinline__ void store4(char* row, int col, const float (&x)[4], 
             if (c < valid) p[c] = Num<T>::from(x[c]);
     }
 }
+
+// Kernels for few rows to a group (csrc/epp_grouped_few.hip); operands as direct loads want them.
+bool few_rows(bool fp32, int64_t m, int G, int N);
+int launch_few(int type, bool input, const GroupedArgs& g, hipStream_t s);
 
 // Kernels of their own for narrow fp32 matrices (csrc/epp_grouped_narrow.hip).
 bool narrow_rows(int K, int N);     // of contraction K onto N columns

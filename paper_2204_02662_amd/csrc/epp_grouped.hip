@@ -54,19 +54,8 @@ __device__ __forceinline__ floatx16 multiply(uintx4 a, uintx4 b, floatx16 c) {
 }
 
 // ---------------------------------------------------------------- operand tiles
-__device__ __forceinline__ unsigned lds_address(const void* p) {
-    return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
-}
-// 16 bytes a lane into LDS, lane after lane from `to` on.  Complete once vmcnt says so (wait_and_meet).  (Not the compiler's builtin: it waits
-// for all of these loads before every transposing LDS read, those of the next tile included.  The compiler writes m0 right before its own uses.)
-__device__ __forceinline__ void load_to_lds(const char* from, unsigned to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
-}
 __device__ __forceinline__ void load4_to_lds(const char* from, unsigned to) {  // (4 bytes a lane)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory");
-}
-__device__ __forceinline__ void load_to_lds(const char* base, unsigned off, unsigned to) {  // (base the same in all lanes)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
 }
 // All loads of this wavefront have arrived and all its LDS reads are done; then the same for the workgroup's.
 __device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -640,6 +629,8 @@ template <class T, int MODE>
 int launch_rows(const GroupedArgs& g, bool direct, hipStream_t s) {
     if constexpr (sizeof(T) == 4)
         if (narrow_rows(MODE == kInput ? g.F_out : g.F_in, MODE == kInput ? g.F_in : g.F_out)) return launch_narrow_rows(MODE == kInput, g, s);
+    if (direct && few_rows(sizeof(T) == 4, g.m, g.G, MODE == kInput ? g.F_in : g.F_out))
+        return launch_few(sizeof(T) == 4 ? EPP_FLOAT32 : std::is_same_v<T, __bf16> ? EPP_BFLOAT16 : EPP_FLOAT16, MODE == kInput, g, s);
     if constexpr (sizeof(T) == 2)
         if (direct && large_tiles(g.m / 256 + g.G / 2, MODE == kInput ? g.F_in : g.F_out)) return launch_rows_of<T, MODE, 2, 4, 4, 2, true, true>(g, s);
     if (direct) return launch_rows_of<T, MODE, 2, 2, 2, 2, true, false>(g, s);
