@@ -29,6 +29,8 @@
 
 using namespace epp_grouped;
 
+#include <cmath>
+
 namespace {
 
 constexpr int kMaxGroups = 2048;
@@ -61,13 +63,14 @@ __device__ __forceinline__ void load4_to_lds(const char* from, unsigned to) {  /
 __device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 __device__ __forceinline__ const char* zeros() { return reinterpret_cast<const char*>(g_zeros); }
-// A piece with `valid` elements (0 .. a piece's), through registers.
+// Pieces through registers.  One that the line's end cuts short is loaded so that it ends there, and shifted into place when it is put into
+// LDS: a load under a condition would be waited for where it stands.  Lines shorter than a piece are loaded element by element.
+typedef unsigned int any_uintx4 __attribute__((ext_vector_type(4), aligned(2)));
+
 template <class T>
-__device__ __forceinline__ uintx4 load_piece(const char* p, int64_t valid) {
+__device__ __forceinline__ uintx4 load_short(const char* p, int valid) {
     constexpr int E = 16 / (int)sizeof(T);
-    typedef unsigned int any_uintx4 __attribute__((ext_vector_type(4), aligned(2)));
     uintx4 v = {0, 0, 0, 0};
-    if (valid >= E) return *reinterpret_cast<const any_uintx4*>(p);
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
@@ -79,6 +82,30 @@ __device__ __forceinline__ uintx4 load_piece(const char* p, int64_t valid) {
     }
     return v;
 }
+// The piece at p, of which `valid` elements are inside its line; zeros for none of them.
+template <class T>
+__device__ __forceinline__ uintx4 load_piece(const char* p, int valid, bool short_line) {
+    constexpr int E = 16 / (int)sizeof(T);
+    if (short_line) return load_short<T>(p, valid);
+    return *reinterpret_cast<const any_uintx4*>(valid <= 0 ? zeros() : valid >= E ? p : p - (E - valid) * (int)sizeof(T));
+}
+__device__ __forceinline__ uintx4 shifted(uintx4 v, int bits) {  // to lower addresses, zeros behind
+    unsigned long long lo = (unsigned long long)v[1] << 32 | v[0], hi = (unsigned long long)v[3] << 32 | v[2];
+    if (bits >= 64) {
+        lo = hi;
+        hi = 0;
+    }
+    const int s = bits & 63;
+    lo = s ? lo >> s | hi << (64 - s) : lo;
+    hi >>= s;
+    return uintx4{(unsigned int)lo, (unsigned int)(lo >> 32), (unsigned int)hi, (unsigned int)(hi >> 32)};
+}
+// What a piece of `valid` elements is to be shifted by.
+template <class T>
+__device__ __forceinline__ int shift_of(int valid, bool short_line) {
+    constexpr int E = 16 / (int)sizeof(T);
+    return valid > 0 && valid < E && !short_line ? (E - valid) * 8 * (int)sizeof(T) : 0;
+}
 
 // Lines of K: TD rows, whose places are set once.  DIRECT: what stands in a line without a row is somebody's numbers (the result's row
 // is not written, or written as zeros); behind the contraction's end there are zeros.
@@ -89,6 +116,8 @@ struct LinesOfK {
     unsigned off[DIRECT ? N : 1];
     const char* p[DIRECT ? 1 : N];
     uintx4 held[DIRECT ? 1 : N];
+    int shift;         // .. by so many bits, once they are here
+    bool cut;          // .. in some lanes
     int k, K;          // the contraction's element in this thread's pieces, and its end
     unsigned lds_wave;
     // place(i): place of tile row i as seen from `from`, -1: none
@@ -114,7 +143,9 @@ struct LinesOfK {
             if (FULL) load_to_lds(base, off[i], at);
             else load_to_lds(k < K ? base + off[i] : zeros(), at);
         } else {
-            held[i] = load_piece<T>(p[i] + (int64_t)k * (int64_t)sizeof(T), p[i] ? K - k : 0);
+            held[i] = load_piece<T>(p[i] + (int64_t)k * (int64_t)sizeof(T), p[i] ? K - k : 0, K < E);
+            shift = shift_of<T>(K - k, K < E);
+            cut = !FULL;
         }
     }
     __device__ __forceinline__ void advance() {  // after all pieces of a tile
@@ -124,7 +155,7 @@ struct LinesOfK {
     __device__ __forceinline__ void put(char* to) {
         if constexpr (!DIRECT) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) *reinterpret_cast<uintx4*>(to + (i * NT + threadIdx.x) * 16) = held[i];
+            for (int i = 0; i < N; ++i) *reinterpret_cast<uintx4*>(to + (i * NT + threadIdx.x) * 16) = cut ? shifted(held[i], shift) : held[i];
         }
     }
     // Piece 2 s + half of rows c0 + l % 32 (c0 a multiple of 32).
@@ -164,6 +195,8 @@ struct LinesOfWidth {
     int32_t row[!DIRECT && LIST ? N : 1];
     unsigned lds_wave;
     uintx4 held[DIRECT ? 1 : N];
+    int shift;          // .. by so many bits, once they are here
+    bool cut;           // .. in some lanes
     __device__ __forceinline__ void start(const Side& side, int64_t first, int64_t end, int c0, int w, int wave, char* lds_ring = nullptr, bool loads_list = false) {
         const int t = threadIdx.x, line = t / kPieces;
         s = side;
@@ -186,7 +219,11 @@ struct LinesOfWidth {
             ask_rows(0);
             ask_rows(1);
         }
-        if constexpr (LIST && !DIRECT) next_rows();
+        if constexpr (!DIRECT) {
+            shift = shift_of<T>(width - c, width < E);
+            cut = c0 + TD > width;
+            if constexpr (LIST) next_rows();
+        }
     }
     // The rows of a tile into slot q of the ring.  (Loaded into registers and kept there from tile to tile, they would have to be waited for
     // behind the operands' loads, which the compiler's count of loads does not know: 594 instead of 380 us for 16 groups of 2,048 entries
@@ -228,7 +265,7 @@ struct LinesOfWidth {
                 if (s.rows) r = row[i];
             }
             const bool no = e >= last || r < 0 || r >= s.n || c >= width;
-            held[i] = load_piece<T>(s.data + r * s.ld + (int64_t)c * (int64_t)sizeof(T), no ? 0 : width - c);
+            held[i] = load_piece<T>(s.data + r * s.ld + (int64_t)c * (int64_t)sizeof(T), no ? 0 : width - c, width < E);
         }
     }
     __device__ __forceinline__ void advance() {
@@ -243,7 +280,7 @@ struct LinesOfWidth {
     __device__ __forceinline__ void put(char* to) {
         if constexpr (!DIRECT) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) *reinterpret_cast<uintx4*>(to + (i * NT + threadIdx.x) * 16) = held[i];
+            for (int i = 0; i < N; ++i) *reinterpret_cast<uintx4*>(to + (i * NT + threadIdx.x) * 16) = cut ? shifted(held[i], shift) : held[i];
         }
     }
     // Piece 2 s + half of the contraction for columns c + l % 32.
@@ -619,6 +656,12 @@ int launch_rows_of(const GroupedArgs& g, hipStream_t s) {
     return EPP_OK;
 }
 
+// Tiles of 64 x 64 where those of 128 x 128 would not be enough for the chip, and for floats always: their products take 16 times as long, so
+// that tiles which are not full, or not there, cost more than fetching.  128 / 64, us: bfloat16, 4 groups, 300 entries, 1,024 x 1,024 (34 tiles)
+// 14.1 / 8.2, 2,000 (141) 15.5 / 13.4, 8,000 (516) 25.3 / 35.4; floats, 300 of 4,096 x 1,024 255 / 77, 16 groups, 8,000 733 / 577,
+// 4 groups, 30,000 1,934 / 1,898.
+bool small_tiles(int64_t tiles) { return tiles < kUnits; }
+
 // 16 bits: tiles of 256 x 256, which fetch half as much a product as tiles of 128 x 128 but come one to a compute unit, where there are enough
 // of them and the width does not waste a part of each.  bfloat16, groups of exponentially distributed sizes, 128 / 256 wide, us: 2,048 entries,
 // 16 groups, 4,096 x 4,096 (about 256 tiles of 256) 173 / 154; 32,768, 32, 4,096 x 2,048 663 / 593; 32,768, 64, 2,048 x 512 (320) 112 / 101;
@@ -627,14 +670,21 @@ bool large_tiles(int64_t rows, int width) { return (width % 256 == 0 || width >=
 
 template <class T, int MODE>
 int launch_rows(const GroupedArgs& g, bool direct, hipStream_t s) {
+    const int N = MODE == kInput ? g.F_in : g.F_out, K = MODE == kInput ? g.F_out : g.F_in;
     if constexpr (sizeof(T) == 4)
-        if (narrow_rows(MODE == kInput ? g.F_out : g.F_in, MODE == kInput ? g.F_in : g.F_out)) return launch_narrow_rows(MODE == kInput, g, s);
-    if (direct && few_rows(sizeof(T) == 4, g.m, g.G, MODE == kInput ? g.F_in : g.F_out))
+        if (narrow_rows(K, N)) return launch_narrow_rows(MODE == kInput, g, s);
+    if (direct && few_rows(sizeof(T) == 4, g.m, g.G, N))
         return launch_few(sizeof(T) == 4 ? EPP_FLOAT32 : std::is_same_v<T, __bf16> ? EPP_BFLOAT16 : EPP_FLOAT16, MODE == kInput, g, s);
     if constexpr (sizeof(T) == 2)
-        if (direct && large_tiles(g.m / 256 + g.G / 2, MODE == kInput ? g.F_in : g.F_out)) return launch_rows_of<T, MODE, 2, 4, 4, 2, true, true>(g, s);
-    if (direct) return launch_rows_of<T, MODE, 2, 2, 2, 2, true, false>(g, s);
-    return launch_rows_of<T, MODE, 2, 2, 2, 2, false, false>(g, s);
+        if (direct && large_tiles(g.m / 256 + g.G / 2, N)) return launch_rows_of<T, MODE, 2, 4, 4, 2, true, true>(g, s);
+    if (sizeof(T) == 4 || small_tiles((g.m / 128 + g.G / 2) * ((N + 127) / 128))) {
+        if (direct) return launch_rows_of<T, MODE, 2, 2, 1, 1, true, false>(g, s);
+        return launch_rows_of<T, MODE, 2, 2, 1, 1, false, false>(g, s);
+    }
+    if constexpr (sizeof(T) == 2) {
+        if (direct) return launch_rows_of<T, MODE, 2, 2, 2, 2, true, false>(g, s);
+        return launch_rows_of<T, MODE, 2, 2, 2, 2, false, false>(g, s);
+    }
 }
 
 // product (X, W -> out) and input gradient (grad_out, W -> grad_X)
@@ -680,11 +730,17 @@ Chunks chunking(bool fp32, int64_t m, int G, int F_in, int F_out) {
         const int64_t per = narrow_weight_chunk(m);
         return {per, std::max<int64_t>(most_tiles(m, G, per), 1)};
     }
-    const int64_t tiles = (int64_t)((F_in + 127) / 128) * ((F_out + 127) / 128);
-    // (groups differ in size: half of them have to fill the chip; chunks of fewer than 512 entries take less time than their partial sums)
-    const int64_t at_once = tiles * ((G + 1) / 2), wanted = (512 + at_once - 1) / at_once;
-    if (wanted <= 1 || m < 512 * (int64_t)G) return {0, G};
-    const int64_t per = std::max<int64_t>((m * 2 / G + wanted - 1) / wanted, 512);
+    // A group's entries are one workgroup's, about 0.7 us a tile of them; groups differ in size, so the longest is taken to have twice the
+    // average.  Cut into n chunks, that takes an n-th, and the partial sums of all chunks are written and read (8 bytes an element at
+    // about 2.7 TB/s) and added by a launch of 5 us.  4 groups, bfloat16, whole / cut, us: 30,000 entries, 1,024 x 1,024 162 / 100;
+    // 2,000 of the same 17 / 32; 2,000, 160 x 100 17.6 / 10.8.
+    const double longest = std::min<double>((double)m, 2.0 * (double)m / G), whole = 0.7 * longest / (fp32 ? 32 : 64);
+    const double each = 0.5 * G * F_in * F_out * 3e-6;
+    const int64_t tiles = (int64_t)((F_in + 63) / 64) * ((F_out + 63) / 64), at_once = tiles * ((G + 1) / 2);
+    const double most = (double)((8 * kUnits + at_once - 1) / at_once);  // (more than eight workgroups to a compute unit gain nothing)
+    const double n = std::min(std::sqrt(whole / each), most);
+    if (n < 2.0 || whole / n + n * each + 5.0 >= whole) return {0, G};
+    const int64_t per = ((int64_t)(longest / n) / 64 + 1) * 64;
     return {per, most_tiles(m, G, per)};
 }
 
@@ -705,9 +761,17 @@ int launch_weight_tiles(const GroupedArgs& g, int64_t chunks, bool direct, hipSt
             if (g.a.rows || g.b.rows) return launch_weight_of<T, TO, 2, 4, 4, 2, true, true>(g, chunks, s);
             return launch_weight_of<T, TO, 2, 4, 4, 2, true, false>(g, chunks, s);
         }
-    if (direct && (g.a.rows || g.b.rows)) return launch_weight_of<T, TO, 2, 2, 2, 2, true, true>(g, chunks, s);
-    if (direct) return launch_weight_of<T, TO, 2, 2, 2, 2, true, false>(g, chunks, s);
-    return launch_weight_of<T, TO, 2, 2, 2, 2, false, true>(g, chunks, s);
+    const bool list = g.a.rows || g.b.rows;
+    if (sizeof(T) == 4 || small_tiles(chunks * ((g.F_in + 127) / 128) * ((g.F_out + 127) / 128))) {
+        if (direct && list) return launch_weight_of<T, TO, 2, 2, 1, 1, true, true>(g, chunks, s);
+        if (direct) return launch_weight_of<T, TO, 2, 2, 1, 1, true, false>(g, chunks, s);
+        return launch_weight_of<T, TO, 2, 2, 1, 1, false, true>(g, chunks, s);
+    }
+    if constexpr (sizeof(T) == 2) {
+        if (direct && list) return launch_weight_of<T, TO, 2, 2, 2, 2, true, true>(g, chunks, s);
+        if (direct) return launch_weight_of<T, TO, 2, 2, 2, 2, true, false>(g, chunks, s);
+        return launch_weight_of<T, TO, 2, 2, 2, 2, false, true>(g, chunks, s);
+    }
 }
 
 template <class TO>

@@ -199,7 +199,7 @@ int launch_type(bool input, const GroupedArgs& g, hipStream_t s) { return input 
 // 256 of the same 39.1 / 31.4; but 64, 2,048 x 4,096 (256) 25.5 / 35.2 and 64 groups, 256, 2,048 x 4,096 201 / 198.  Floats: 8 groups, 16
 // entries, 4,096 x 1,024 250 / 27; 64 groups, 1,024, 2,048 x 4,096 980 / 604; 2,048 of the same 1,077 / 1,105.
 bool epp_grouped::few_rows(bool fp32, int64_t m, int G, int N) {
-    if (m >= 32 * (int64_t)G) return false;
+    if (m >= (fp32 ? 24 : 32) * (int64_t)G) return false;
     return fp32 || std::min<int64_t>(G, m) * ((N + 127) / 128) < kUnits;
 }
 
