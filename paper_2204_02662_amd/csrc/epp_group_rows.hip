@@ -1,8 +1,9 @@
 // Entries brought into the order of their groups (a counting sort that keeps the order of a group's entries): what the grouped
 // products need of a router's choices, or of the types of a graph's active vertices.
 //
-// Few entries: one workgroup counts, sums and places them.  Many: blocks of consecutive entries are counted, a wavefront per
-// group sums its counts over the blocks, and the blocks place their entries.  A wavefront finds an entry's rank among its 64 by
+// Few entries: one workgroup counts, sums and places them.  Many: blocks of consecutive entries are counted, and then place their
+// entries; the counts of the blocks before are added up by every block itself where they are few, else by a wavefront per group in a
+// launch between.  A wavefront finds an entry's rank among its 64 by
 // ballots over the bits of the group's number; nothing depends on the order in which blocks or wavefronts run.
 // Group G stands for "no group": its entries come last.
 
@@ -11,8 +12,11 @@
 namespace {
 
 constexpr int kMaxGroups = 2048;
-constexpr int kFew = 8192, kFewGroups = 512, kFewWaves = 16;
+constexpr int kFew = 8192, kFewWaves = 16;
 constexpr int kWaves = 4, kBlockEntries = 2048, kMostBlocks = 1024;
+// Groups whose counts every block adds up itself, one after the other, instead of a launch of its own: 100,000 entries, 8 groups, 9.9 us with two
+// launches; 20,000, 256 groups, 45 us with two, 14 with three.
+constexpr int kFewSums = 32;
 
 struct GroupRowsArgs {
     const int32_t* group_of;
@@ -20,30 +24,46 @@ struct GroupRowsArgs {
     int64_t n, m, per;    // per: entries to a block
     int G, bits, blocks;
     int32_t *offsets, *order;
-    int32_t *counts, *totals;  // counts[group][block], totals[group]
+    int32_t *counts, *totals;  // counts[group][block], totals[group] (NULL: counts are few, and not yet summed over the blocks)
 };
 
-__device__ __forceinline__ int group_at(const GroupRowsArgs& a, int64_t i, int32_t* row) {
-    const int64_t r = a.rows ? (int64_t)a.rows[i] : i;
-    *row = (int32_t)r;
-    const int g = r >= 0 && r < a.n ? a.group_of[r] : -1;
-    return g >= 0 && g < a.G ? g : a.G;
+// f(entry, row, group) for the entries [first, last) of the calling wavefront, 64 at a time, in order, with the numbers of kAhead times 64
+// entries on their way together (their rows first, then their groups).
+template <class F>
+__device__ __forceinline__ void for_entries(const GroupRowsArgs& a, int64_t first, int64_t last, F f) {
+    constexpr int kAhead = 8;
+    const int lane = threadIdx.x & 63;
+    for (int64_t i0 = first; i0 < last; i0 += 64 * kAhead) {
+        int32_t row[kAhead], group[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int64_t i = min(i0 + 64 * j + lane, last - 1);
+            row[j] = a.rows ? a.rows[i] : (int32_t)i;
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const bool there = row[j] >= 0 && row[j] < a.n;
+            group[j] = there ? a.group_of[row[j]] : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int g = group[j] >= 0 && group[j] < a.G ? group[j] : a.G;
+            if (i0 + 64 * j < last) f(i0 + 64 * j + lane < last, row[j], g);
+        }
+    }
 }
 
 // Adds the group counts of entries [first, last) to count[], by the calling wavefront.
 __device__ __forceinline__ void count_entries(const GroupRowsArgs& a, int64_t first, int64_t last, int32_t* count) {
-    int32_t row;
-    for (int64_t i = first + (threadIdx.x & 63); i < last; i += 64) atomicAdd(&count[group_at(a, i, &row)], 1);
+    for_entries(a, first, last, [&](bool have, int32_t, int g) {
+        if (have) atomicAdd(&count[g], 1);
+    });
 }
 
 // Places entries [first, last) from next[] on, by the calling wavefront, which owns next[].
 __device__ __forceinline__ void place_entries(const GroupRowsArgs& a, int64_t first, int64_t last, volatile int32_t* next) {
     const int lane = threadIdx.x & 63;
-    for (int64_t i0 = first; i0 < last; i0 += 64) {
-        const int64_t i = i0 + lane;
-        const bool have = i < last;
-        int32_t row = 0;
-        const int g = have ? group_at(a, i, &row) : 0;
+    for_entries(a, first, last, [&](bool have, int32_t row, int g) {
         unsigned long long same = __ballot(have);
         for (int b = 0; b < a.bits; ++b) {
             const unsigned long long set = __ballot((g >> b) & 1);
@@ -57,11 +77,10 @@ __device__ __forceinline__ void place_entries(const GroupRowsArgs& a, int64_t fi
             __builtin_amdgcn_wave_barrier();
             a.order[at + rank] = row;
         }
-    }
+    });
 }
 
-// Exclusive sums over `n` values in LDS (n <= 4 * threads of the workgroup's first wavefronts is not needed: one wavefront goes
-// through them 64 at a time).  Called by one wavefront; returns the sum of all.
+// Exclusive sums over `n` values, 64 at a time, by one wavefront.  Returns the sum of all.
 __device__ __forceinline__ int32_t exclusive_sums(int32_t* v, int n) {
     const int lane = threadIdx.x & 63;
     int32_t before = 0;
@@ -80,9 +99,10 @@ __device__ __forceinline__ int32_t exclusive_sums(int32_t* v, int n) {
     return before;
 }
 
+template <int MOST>  // groups
 __global__ __launch_bounds__(64 * kFewWaves) void k_group_few(GroupRowsArgs a) {
-    __shared__ int32_t next[kFewWaves][kFewGroups + 1];
-    __shared__ int32_t begin[kFewGroups + 1];
+    __shared__ int32_t next[kFewWaves][MOST + 1];
+    __shared__ int32_t begin[MOST + 1];
     const int t = threadIdx.x, w = t >> 6, groups = a.G + 1;
     for (int i = t; i < kFewWaves * groups; i += 64 * kFewWaves) next[i / groups][i % groups] = 0;
     __syncthreads();
@@ -127,29 +147,38 @@ __global__ __launch_bounds__(64 * kWaves) void k_group_count(GroupRowsArgs a) {
 
 // A wavefront per group: the sums of its counts up to every block, and of all.
 __global__ __launch_bounds__(64) void k_group_sums(GroupRowsArgs a) {
-    const int lane = threadIdx.x;
-    int32_t* c = a.counts + (int64_t)blockIdx.x * a.blocks;
-    int32_t before = 0;
-    for (int i0 = 0; i0 < a.blocks; i0 += 64) {
-        const int i = i0 + lane;
-        const int32_t mine = i < a.blocks ? c[i] : 0;
-        int32_t upto = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int32_t x = __shfl_up(upto, d, 64);
-            if (lane >= d) upto += x;
-        }
-        if (i < a.blocks) c[i] = before + upto - mine;
-        before += __shfl(upto, 63, 64);
-    }
-    if (lane == 0) a.totals[blockIdx.x] = before;
+    const int32_t total = exclusive_sums(a.counts + (int64_t)blockIdx.x * a.blocks, a.blocks);
+    if (threadIdx.x == 0) a.totals[blockIdx.x] = total;
 }
 
 __global__ __launch_bounds__(64 * kWaves) void k_group_place(GroupRowsArgs a) {
     extern __shared__ int32_t next[];  // [wavefront][group], and before that the groups' beginnings in the first row
+    __shared__ int32_t before_here[kFewSums + 1];
     const int t = threadIdx.x, w = t >> 6, groups = a.G + 1;
-    for (int i = t; i < groups; i += 64 * kWaves) next[i] = a.totals[i];
     for (int i = groups + t; i < kWaves * groups; i += 64 * kWaves) next[i] = 0;
+    if (a.totals) {
+        for (int i = t; i < groups; i += 64 * kWaves) next[i] = a.totals[i];
+    } else {  // few counts: every block adds them up itself (the second row of next[]: those of the blocks before)
+        const int lane = t & 63;
+        for (int g = w; g < groups; g += kWaves) {
+            int32_t before = 0, all = 0;
+#pragma unroll 8
+            for (int i = lane; i < a.blocks; i += 64) {
+                const int32_t c = a.counts[g * a.blocks + i];
+                all += c;
+                if (i < (int)blockIdx.x) before += c;
+            }
+#pragma unroll
+            for (int d = 32; d; d /= 2) {
+                before += __shfl_xor(before, d, 64);
+                all += __shfl_xor(all, d, 64);
+            }
+            if (lane == 0) {
+                next[g] = all;
+                before_here[g] = before;
+            }
+        }
+    }
     __syncthreads();
     if (w == 0) exclusive_sums(next, groups);
     __syncthreads();
@@ -161,7 +190,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_group_place(GroupRowsArgs a) {
     if (w + 1 < kWaves) count_entries(a, mine, last, next + (w + 1) * groups);
     __syncthreads();
     for (int g = t; g < groups; g += 64 * kWaves) {
-        int32_t sum = next[g] + a.counts[(int64_t)g * a.blocks + blockIdx.x];
+        int32_t sum = next[g] + (a.totals ? a.counts[(int64_t)g * a.blocks + blockIdx.x] : before_here[g]);
         next[g] = sum;
 #pragma unroll
         for (int x = 1; x < kWaves; ++x) {
@@ -180,7 +209,7 @@ int check(int64_t m, int G) {
     if (G > kMaxGroups) { epp_set_error("%d groups (up to %d)", G, kMaxGroups); return EPP_ERR_TOO_LARGE; }
     return EPP_OK;
 }
-bool few(int64_t m, int G) { return m <= kFew && G <= kFewGroups; }
+bool few(int64_t m) { return m <= kFew; }
 // Entries to a block: enough blocks to fill the chip, and not so many that their counts would be what takes time.
 int64_t block_entries(int64_t m) {
     const int64_t least = (m + kMostBlocks - 1) / kMostBlocks;
@@ -191,7 +220,7 @@ int64_t block_entries(int64_t m) {
 
 extern "C" int64_t epp_group_rows_workspace(int64_t m, int G) {
     EPP_TRY(check(m, G));
-    if (few(m, G)) return 16;
+    if (few(m)) return 16;
     const int64_t per = block_entries(m), blocks = (m + per - 1) / per;
     return (std::max<int64_t>(blocks, 1) + 1) * ((int64_t)G + 1) * 4;
 }
@@ -230,19 +259,23 @@ extern "C" int epp_group_rows(const int32_t* group_of, int64_t n, const int32_t*
     a.offsets = offsets;
     a.order = order;
     hipStream_t s = (hipStream_t)stream;
-    if (few(m, G)) {
-        hipLaunchKernelGGL(k_group_few, dim3(1), dim3(64 * kFewWaves), 0, s, a);
+    if (few(m)) {
+        if (G <= 256) hipLaunchKernelGGL((k_group_few<256>), dim3(1), dim3(64 * kFewWaves), 0, s, a);
+        else hipLaunchKernelGGL((k_group_few<kMaxGroups>), dim3(1), dim3(64 * kFewWaves), 0, s, a);
         EPP_HIP_TRY(hipGetLastError());
         return EPP_OK;
     }
     a.per = block_entries(m);
     a.blocks = (int)std::max<int64_t>((m + a.per - 1) / a.per, 1);
     a.counts = static_cast<int32_t*>(workspace);
-    a.totals = a.counts + (int64_t)a.blocks * (G + 1);
+    const bool sums = G > kFewSums;
+    if (sums) a.totals = a.counts + (int64_t)a.blocks * (G + 1);
     hipLaunchKernelGGL(k_group_count, dim3((unsigned)a.blocks), dim3(64 * kWaves), (size_t)(G + 1) * 4, s, a);
     EPP_HIP_TRY(hipGetLastError());
-    hipLaunchKernelGGL(k_group_sums, dim3((unsigned)(G + 1)), dim3(64), 0, s, a);
-    EPP_HIP_TRY(hipGetLastError());
+    if (sums) {
+        hipLaunchKernelGGL(k_group_sums, dim3((unsigned)(G + 1)), dim3(64), 0, s, a);
+        EPP_HIP_TRY(hipGetLastError());
+    }
     hipLaunchKernelGGL(k_group_place, dim3((unsigned)a.blocks), dim3(64 * kWaves), (size_t)kWaves * (size_t)(G + 1) * 4, s, a);
     EPP_HIP_TRY(hipGetLastError());
     return EPP_OK;

@@ -132,6 +132,16 @@ def test_large_small_and_no_numbers():
         assert math.isnan(norm.item()) and torch.isnan(g).all()
 
 
+def test_an_infinite_bound_leaves_everything():
+    """Infinities as well: nothing is scaled, in place or not."""
+    for n in (300, 100_000):
+        g = randn(n, seed=n)
+        g[7], g[-1] = float("inf"), float("-inf")
+        norm, ws, out = torch.empty(1, device=dev()), workspace(1), torch.empty_like(g)
+        epp.epp_clip_gradients([g], math.inf, norm, ws, out=[out])
+        assert math.isinf(norm.item()) and torch.equal(out, g)
+
+
 def test_a_gradient_twice():
     """Counts twice in the norm; scaling it twice has no meaning and is refused, as is an output on another's memory."""
     g, h = randn(100, seed=1), randn(100, seed=2)
