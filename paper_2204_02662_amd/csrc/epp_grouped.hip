@@ -60,7 +60,9 @@ __device__ __forceinline__ void load4_to_lds(const char* from, unsigned to) {  /
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory");
 }
 // All loads of this wavefront have arrived and all its LDS reads are done; then the same for the workgroup's.
-__device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// (ALLOWED: but for the last so many loads)
+template <int ALLOWED>
+__device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(ALLOWED) : "memory"); }
 
 __device__ __forceinline__ const char* zeros() { return reinterpret_cast<const char*>(g_zeros); }
 // Pieces through registers.  One that the line's end cuts short is loaded so that it ends there, and shifted into place when it is put into
@@ -111,7 +113,9 @@ __device__ __forceinline__ int shift_of(int valid, bool short_line) {
 // is not written, or written as zeros); behind the contraction's end there are zeros.
 template <class T, int TD, int NT, bool DIRECT>
 struct LinesOfK {
-    static constexpr int E = 16 / (int)sizeof(T), N = TD * 8 / NT, kBytes = TD * kLine, kSteps = kLine / (int)sizeof(T);
+    static constexpr int E = 16 / (int)sizeof(T), kPieces = kLine / 16, N = TD * kPieces / NT, kBytes = TD * kLine, kSteps = kLine / (int)sizeof(T);
+    static __device__ __forceinline__ int turn(int row) { return (row >> 1) & 7; }  // what a line's pieces are permuted by
+    static_assert((NT / kPieces) % 16 == 0, "all of a thread's pieces are of the same part of their lines");
     const char* base;  // DIRECT: the same for all lanes, moves with the contraction
     unsigned off[DIRECT ? N : 1];
     const char* p[DIRECT ? 1 : N];
@@ -124,12 +128,12 @@ struct LinesOfK {
     template <class F> __device__ __forceinline__ void start(const char* from, int end, int wave, F place) {
         const int t = threadIdx.x;
         K = end;
-        k = ((t & 7) ^ ((t >> 4) & 7)) * E;
+        k = ((t % kPieces) ^ turn(t / kPieces)) * E;
         base = uniform(from);
         lds_wave = (unsigned)wave * 1024u;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int64_t at = place((i * NT + t) >> 3);
+            const int64_t at = place((i * NT + t) / kPieces);
             if constexpr (DIRECT) off[i] = (unsigned)(at < 0 ? 0 : at) + (unsigned)k * (unsigned)sizeof(T);
             else p[i] = at < 0 ? nullptr : from + at;
         }
@@ -161,7 +165,7 @@ struct LinesOfK {
     // Piece 2 s + half of rows c0 + l % 32 (c0 a multiple of 32).
     static __device__ __forceinline__ uintx4 piece(const char* tile, int c0, int s) {
         const int l = threadIdx.x & 63;
-        return *reinterpret_cast<const uintx4*>(tile + (c0 + (l & 31)) * kLine + (((2 * s + (l >> 5)) ^ ((l >> 1) & 7)) * 16));
+        return *reinterpret_cast<const uintx4*>(tile + (c0 + (l & 31)) * kLine + (((2 * s + (l >> 5)) ^ turn(l & 31)) * 16));
     }
 };
 
@@ -169,7 +173,7 @@ struct LinesOfK {
 // rows through a list.
 template <class T, int TD, int NT, bool DIRECT, bool LIST>
 struct LinesOfWidth {
-    static constexpr int E = 16 / (int)sizeof(T), N = TD * 8 / NT, kBytes = TD * kLine;
+    static constexpr int E = 16 / (int)sizeof(T), N = TD * kLine / 16 / NT, kBytes = TD * kLine;
     static constexpr int kWide = TD * (int)sizeof(T), kPieces = kWide / 16, kPairs = kWide / 32;
     static constexpr int kSteps = kLine / (int)sizeof(T);
     static_assert(NT % kPieces == 0 && (kPairs == 4 || kPairs % 8 == 0), "tile");
@@ -318,12 +322,13 @@ struct Place {
 };
 
 // One tile: WM x WN wavefronts, each with BM x BN blocks of 32 x 32 of the result.  TO: type of the results.
-template <class T, class TO, int MODE, int WM, int WN, int BM, int BN, bool DIRECT, bool LIST>
+template <class T, class TO, int MODE, int WM, int WN, int BM, int BN, bool DIRECT, bool LIST, int STAGES>
 __device__ __forceinline__ void form_tile(const GroupedArgs& g, const Place& at, char* lds) {
     constexpr int NT = 64 * WM * WN, TM = 32 * WM * BM, TN = 32 * WN * BN;
     using A = std::conditional_t<MODE == kWeight, LinesOfWidth<T, TM, NT, DIRECT, LIST>, LinesOfK<T, TM, NT, DIRECT>>;
     using B = std::conditional_t<MODE == kInput, LinesOfK<T, TN, NT, DIRECT>, LinesOfWidth<T, TN, NT, DIRECT, LIST>>;
-    constexpr int kBytes = A::kBytes + B::kBytes, kSteps = kLine / (int)sizeof(T);
+    constexpr int kBytes = A::kBytes + B::kBytes, kSteps = kLine / (int)sizeof(T), kSubs = kLine / 32, kLoads = A::N + B::N;
+    static_assert(STAGES == 2 || (DIRECT && !LIST && kLoads * (STAGES - 1) < 64), "stages");
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wn = w % WN, wm = w / WN;
     A a;
     B b;
@@ -343,10 +348,10 @@ __device__ __forceinline__ void form_tile(const GroupedArgs& g, const Place& at,
         else b.start(Side{W, K, ldw, nullptr}, 0, K, n0, N, w);
     } else {
         K = at.last - at.first;
-        char* ring = lds + 2 * kBytes;
+        char* ring = lds + STAGES * kBytes;
         a.start(g.a, at.first, at.last, (int)m0, g.F_in, w, ring, w == 0);
         b.start(g.b, at.first, at.last, n0, g.F_out, w, ring + 1024, w == 1);
-        if (DIRECT && LIST) wait_and_meet();
+        if (DIRECT && LIST) wait_and_meet<0>();
     }
 
     // Two sets of operand pieces in registers: while the matrix cores work on one, the other is read.  The wavefronts meet when all have
@@ -392,37 +397,47 @@ __device__ __forceinline__ void form_tile(const GroupedArgs& g, const Place& at,
         prepare();
         fetch_all(No{}, lds);
         put(lds);
-        wait_and_meet();
-        if (steps > 1) {
+        if constexpr (STAGES > 2) {
+#pragma unroll
+            for (int i = 1; i < STAGES - 1; ++i)
+                if (i < steps) fetch_all(No{}, lds + i * kBytes);
+        }
+        if (STAGES > 2 && steps >= STAGES - 1) wait_and_meet<kLoads * (STAGES - 2)>();
+        else wait_and_meet<0>();
+        if (STAGES - 1 < steps) {
             prepare();
-            fetch_all(No{}, lds + kBytes);
+            fetch_all(No{}, lds + (STAGES - 1) * kBytes);
         }
     }
     auto contract = [&](auto live) {
         int64_t st = 0;
+        int stage = 0;
         if (live && steps > 0) read(lds, 0, 0);
-        auto step = [&](auto middle) {  // middle: the next but one tile is a full one
-            char* now = lds + (st & 1) * kBytes;
-            char* next = lds + ((st & 1) ^ 1) * kBytes;
+        auto step = [&](auto middle) {  // middle: the tile to be loaded into this one's place is a full one
+            char* now = lds + stage * kBytes;
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
+            char* next = lds + stage * kBytes;
             if constexpr (live) read(now, 1, 1);
-            if (middle || st + 2 < steps) prepare();
+            if (middle || st + STAGES < steps) prepare();
             if constexpr (live) {
-                work(0);
-                read(now, 2, 0);
-                work(1);
-                read(now, 3, 1);
-                work(0);
+#pragma unroll
+                for (int s = 1; s < kSubs; ++s) {
+                    work((s - 1) & 1);
+                    if (s + 1 < kSubs) read(now, s + 1, (s + 1) & 1);
+                }
             }
             if (!DIRECT && (middle || st + 1 < steps)) put(next);
-            wait_and_meet();
+            // (of the loads that are on their way, the next tile's have to have arrived)
+            if constexpr (middle) wait_and_meet<kLoads * (STAGES - 2)>();
+            else wait_and_meet<0>();
             if constexpr (middle) fetch_all(Yes{}, now);
-            else if (st + 2 < steps) fetch_all(No{}, now);
+            else if (st + STAGES < steps) fetch_all(No{}, now);
             if constexpr (live) {
                 if (middle || st + 1 < steps) read(next, 0, 0);
                 work(1);
             }
         };
-        for (; st + 2 < full; ++st) step(Yes{});
+        for (; st + STAGES < full; ++st) step(Yes{});
         for (; st < steps; ++st) step(No{});
     };
     // (a wavefront whose rows lie behind the group's last has nothing to do but its share of the loads)
@@ -455,10 +470,10 @@ __device__ __forceinline__ void form_tile(const GroupedArgs& g, const Place& at,
 
 // Product and input gradient.  QUARTERS: where the tiles fill the chip's kUnits compute units some times over and then up to half of them
 // once more, those last tiles are dealt out in quarters.
-template <class T, int MODE, int WM, int WN, int BM, int BN, bool DIRECT, bool QUARTERS>
+template <class T, int MODE, int WM, int WN, int BM, int BN, bool DIRECT, bool QUARTERS, int STAGES>
 __global__ __launch_bounds__(64 * WM * WN) void k_grouped_rows(GroupedArgs g) {
     constexpr int TM = 32 * WM * BM, TN = 32 * WN * BN;
-    __shared__ __attribute__((aligned(128))) char lds[2 * (TM + TN) * kLine];
+    __shared__ __attribute__((aligned(128))) char lds[STAGES * (TM + TN) * kLine];
     const int N = MODE == kInput ? g.F_in : g.F_out;
     const int nt = (N + TN - 1) / TN;
     int64_t tiles;
@@ -481,18 +496,18 @@ __global__ __launch_bounds__(64 * WM * WN) void k_grouped_rows(GroupedArgs g) {
     const Span s = find_group(g.offsets, g.G, g.m, TM, mine / nt, &unused);
     Place at = {s.g, uniform(s.first + (mine / nt - s.chunk0) * TM), uniform(s.last), __builtin_amdgcn_readfirstlane((int)(mine % nt) * TN), 0, 0, const_cast<char*>(g.out.data)};
     if (!QUARTERS || quarter < 0) {
-        form_tile<T, T, MODE, WM, WN, BM, BN, DIRECT, false>(g, at, lds);
+        form_tile<T, T, MODE, WM, WN, BM, BN, DIRECT, false, STAGES>(g, at, lds);
     } else if constexpr (QUARTERS) {
         at.m0 += (quarter & 1) * (TM / 2);
         at.n0 += (quarter >> 1) * (TN / 2);
-        if (at.m0 < at.m_end && at.n0 < N) form_tile<T, T, MODE, WM, WN, BM / 2, BN / 2, DIRECT, false>(g, at, lds);
+        if (at.m0 < at.m_end && at.n0 < N) form_tile<T, T, MODE, WM, WN, BM / 2, BN / 2, DIRECT, false, STAGES>(g, at, lds);
     }
 }
 
-template <class T, class TO, int WM, int WN, int BM, int BN, bool DIRECT, bool LIST>
+template <class T, class TO, int WM, int WN, int BM, int BN, bool DIRECT, bool LIST, int STAGES>
 __global__ __launch_bounds__(64 * WM * WN) void k_grouped_weight(GroupedArgs g) {
     constexpr int TM = 32 * WM * BM, TN = 32 * WN * BN;
-    __shared__ __attribute__((aligned(128))) char lds[2 * (TM + TN) * kLine + (DIRECT && LIST ? 2048 : 0)];
+    __shared__ __attribute__((aligned(128))) char lds[STAGES * (TM + TN) * kLine + (DIRECT && LIST ? 2048 : 0)];
     const int mt = (g.F_in + TM - 1) / TM, nt = (g.F_out + TN - 1) / TN;
     // (the tiles of one group or chunk are dealt to all XCDs: groups differ in size)
     const int per_group = mt * nt, in = (int)(blockIdx.x % per_group), share = per_group / 8;
@@ -511,7 +526,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_grouped_weight(GroupedArgs g) 
         at.last = max(at.first, min((int64_t)g.offsets[chunk + 1], g.m));
         at.out += chunk * g.F_in * g.F_out * (int64_t)sizeof(TO);
     }
-    form_tile<T, TO, kWeight, WM, WN, BM, BN, DIRECT, LIST>(g, at, lds);
+    form_tile<T, TO, kWeight, WM, WN, BM, BN, DIRECT, LIST, STAGES>(g, at, lds);
 }
 
 // grad_W[g] = the sum of its chunks' partial sums, in order (none: zeros).  Four elements to a thread; SLICES threads share the chunks of
@@ -644,14 +659,14 @@ int64_t most_tiles(int64_t m, int64_t G, int64_t tile) { return (m + std::min(G,
 
 int too_many(int64_t blocks) { epp_set_error("%lld workgroups in one launch", (long long)blocks); return EPP_ERR_TOO_LARGE; }
 
-template <class T, int MODE, int WM, int WN, int BM, int BN, bool DIRECT, bool QUARTERS>
+template <class T, int MODE, int WM, int WN, int BM, int BN, bool DIRECT, bool QUARTERS, int STAGES = 2>
 int launch_rows_of(const GroupedArgs& g, hipStream_t s) {
     constexpr int TM = 32 * WM * BM, TN = 32 * WN * BN;
     const int N = MODE == kInput ? g.F_in : g.F_out;
     int64_t blocks = most_tiles(g.m, g.G, TM) * ((N + TN - 1) / TN) + 16;
     if (QUARTERS) blocks += 3 * (kUnits / 2);
     if (blocks > 0x7FFFFFFF) return too_many(blocks);
-    hipLaunchKernelGGL((k_grouped_rows<T, MODE, WM, WN, BM, BN, DIRECT, QUARTERS>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, g);
+    hipLaunchKernelGGL((k_grouped_rows<T, MODE, WM, WN, BM, BN, DIRECT, QUARTERS, STAGES>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, g);
     EPP_HIP_TRY(hipGetLastError());
     return EPP_OK;
 }
@@ -659,7 +674,8 @@ int launch_rows_of(const GroupedArgs& g, hipStream_t s) {
 // Tiles of 64 x 64 where those of 128 x 128 would not be enough for the chip, and for floats always: their products take 16 times as long, so
 // that tiles which are not full, or not there, cost more than fetching.  128 / 64, us: bfloat16, 4 groups, 300 entries, 1,024 x 1,024 (34 tiles)
 // 14.1 / 8.2, 2,000 (141) 15.5 / 13.4, 8,000 (516) 25.3 / 35.4; floats, 300 of 4,096 x 1,024 255 / 77, 16 groups, 8,000 733 / 577,
-// 4 groups, 30,000 1,934 / 1,898.
+// 4 groups, 30,000 1,934 / 1,898.  With less than one of them to a compute unit, four of their tiles of operands in LDS (16 bits: floats work
+// longer on a tile than it takes to load): 4 groups, 300 of 4,096 x 1,024 31.4 / 18.7.
 bool small_tiles(int64_t tiles) { return tiles < kUnits; }
 
 // 16 bits: tiles of 256 x 256, which fetch half as much a product as tiles of 128 x 128 but come one to a compute unit, where there are enough
@@ -678,6 +694,8 @@ int launch_rows(const GroupedArgs& g, bool direct, hipStream_t s) {
     if constexpr (sizeof(T) == 2)
         if (direct && large_tiles(g.m / 256 + g.G / 2, N)) return launch_rows_of<T, MODE, 2, 4, 4, 2, true, true>(g, s);
     if (sizeof(T) == 4 || small_tiles((g.m / 128 + g.G / 2) * ((N + 127) / 128))) {
+        if constexpr (sizeof(T) == 2)
+            if (direct && (g.m / 64 + g.G / 2) * ((N + 63) / 64) <= kUnits) return launch_rows_of<T, MODE, 2, 2, 1, 1, true, false, 4>(g, s);
         if (direct) return launch_rows_of<T, MODE, 2, 2, 1, 1, true, false>(g, s);
         return launch_rows_of<T, MODE, 2, 2, 1, 1, false, false>(g, s);
     }
@@ -744,12 +762,12 @@ Chunks chunking(bool fp32, int64_t m, int G, int F_in, int F_out) {
     return {per, most_tiles(m, G, per)};
 }
 
-template <class T, class TO, int WM, int WN, int BM, int BN, bool DIRECT, bool LIST>
+template <class T, class TO, int WM, int WN, int BM, int BN, bool DIRECT, bool LIST, int STAGES = 2>
 int launch_weight_of(const GroupedArgs& g, int64_t chunks, hipStream_t s) {
     constexpr int TM = 32 * WM * BM, TN = 32 * WN * BN;
     const int64_t blocks = chunks * ((g.F_in + TM - 1) / TM) * ((g.F_out + TN - 1) / TN);
     if (blocks > 0x7FFFFFFF) return too_many(blocks);
-    hipLaunchKernelGGL((k_grouped_weight<T, TO, WM, WN, BM, BN, DIRECT, LIST>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, g);
+    hipLaunchKernelGGL((k_grouped_weight<T, TO, WM, WN, BM, BN, DIRECT, LIST, STAGES>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, g);
     EPP_HIP_TRY(hipGetLastError());
     return EPP_OK;
 }
