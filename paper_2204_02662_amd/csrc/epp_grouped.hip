@@ -504,6 +504,19 @@ __global__ __launch_bounds__(64 * WM * WN) void k_grouped_rows(GroupedArgs g) {
     }
 }
 
+// The group (of up to 64) that `rank` others precede in the order of their sizes, largest first.
+__device__ __forceinline__ int group_of_rank(const int32_t* __restrict__ offsets, int G, int64_t m, int rank) {
+    const int lane = threadIdx.x & 63;
+    const int g = min(lane, G - 1);
+    const int lo = (int)min(max((int64_t)offsets[g], (int64_t)0), m), hi = (int)min(max((int64_t)offsets[g + 1], (int64_t)0), m);
+    // (one number to compare: the size, to 2^-25 of all entries, and before others of the same size the lower group)
+    const int shift = max(0, 39 - __builtin_clzll((unsigned long long)m | 1));
+    const unsigned key = lane < G ? ((unsigned)max(hi - lo, 0) >> shift) * 64u + (63u - (unsigned)lane) : 0u;
+    int before = 0;
+    for (int j = 0; j < G; ++j) before += (unsigned)__builtin_amdgcn_readlane((int)key, j) > key;
+    return __ffsll((long long)__ballot(lane < G && before == rank)) - 1;
+}
+
 template <class T, class TO, int WM, int WN, int BM, int BN, bool DIRECT, bool LIST, int STAGES>
 __global__ __launch_bounds__(64 * WM * WN) void k_grouped_weight(GroupedArgs g) {
     constexpr int TM = 32 * WM * BM, TN = 32 * WN * BN;
@@ -511,7 +524,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_grouped_weight(GroupedArgs g) 
     const int mt = (g.F_in + TM - 1) / TM, nt = (g.F_out + TN - 1) / TN;
     // (the tiles of one group or chunk are dealt to all XCDs: groups differ in size)
     const int per_group = mt * nt, in = (int)(blockIdx.x % per_group), share = per_group / 8;
-    const int64_t chunk = blockIdx.x / per_group;
+    int64_t chunk = blockIdx.x / per_group;
+    if constexpr (BM * BN >= 8) {
+        // (large tiles, a few to a compute unit: the longest groups first, or the last ones to begin end long after the others)
+        if (!g.per && g.G <= 64) chunk = group_of_rank(g.offsets, g.G, g.m, (int)chunk);
+    }
     const int tile = per_group % 8 == 0 ? (in & 7) * share + (in >> 3) : in;
     Place at = {0, (int64_t)(tile / nt) * TM, g.F_in, (tile % nt) * TN, 0, 0, const_cast<char*>(g.out.data)};
     if (g.per) {

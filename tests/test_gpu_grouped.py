@@ -147,6 +147,26 @@ def test_many_rows(dtype):
     assert_sums(got, want, size, terms + 520)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_large_tiles(dtype):
+    """Enough tiles of 256 x 256 for the chip, the last ones in quarters or not; contractions that end inside a tile of operands, rows that
+    end inside a tile of the result; weights of large matrices, the longest groups first."""
+    for sizes in ([700, 0, 300, 1, 255, 257, 600, 900], [2_000, 2_100, 0, 1_900], [513] * 9):
+        run_rows(sizes, 200, 4_096, dtype, False, 25)
+        run_rows(sizes, 4_104, 328, dtype, True, 26)
+    sizes, Fi, Fo = [100, 0, 31, 300, 64, 1, 65, 100], 1_544, 4_096
+    m, offsets = sum(sizes), offsets_of(sizes)
+    x, d = randn(m + 20, Fi, seed=27, dtype=dtype), randn(m, Fo, seed=28, dtype=dtype)
+    rows = torch.randperm(m + 20, generator=torch.Generator().manual_seed(3))[:m].int().to(dev())
+    rows[50] = -1
+    ws = torch.empty(epp.epp_grouped_weight_gradient_workspace(m, 8, Fi, Fo), dtype=torch.uint8, device=dev())
+    got = torch.empty(8, Fi, Fo, dtype=dtype, device=dev())
+    for x_rows in (None, rows):
+        epp.epp_grouped_weight_gradient(x[:m] if x_rows is None else x, d, offsets, got, ws, x_rows=x_rows)
+        want, size, terms = weight_gradient(x, d, offsets, m, x_rows)
+        assert_sums(got, want, size, terms)
+
+
 def test_offsets_that_are_not_as_they_should_be():
     """Falling, negative and too large ones: unspecified results in the rows, nothing outside them."""
     x, W = randn(100, 24, seed=31, dtype=torch.bfloat16), randn(4, 24, 40, seed=32, dtype=torch.bfloat16)
