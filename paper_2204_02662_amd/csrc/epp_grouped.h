@@ -122,9 +122,9 @@ bool few_rows(bool fp32, int64_t m, int G, int N);
 int launch_few(int type, bool input, const GroupedArgs& g, hipStream_t s);
 
 // Kernels of their own for narrow fp32 matrices (csrc/epp_grouped_narrow.hip).
-bool narrow_rows(int K, int N);     // of contraction K onto N columns
+bool narrow_rows(int64_t m, int K, int N);  // of contraction K onto N columns
 int launch_narrow_rows(bool input, const GroupedArgs& g, hipStream_t s);
-bool narrow_weight(int F_in, int F_out);
+bool narrow_weight(int64_t m, int F_in, int F_out);
 int64_t narrow_weight_chunk(int64_t m);  // entries to a chunk of partial sums
 int launch_narrow_weight(const GroupedArgs& g, int64_t chunks, hipStream_t s);
 

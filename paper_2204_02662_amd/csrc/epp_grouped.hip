@@ -705,7 +705,7 @@ template <class T, int MODE>
 int launch_rows(const GroupedArgs& g, bool direct, hipStream_t s) {
     const int N = MODE == kInput ? g.F_in : g.F_out, K = MODE == kInput ? g.F_out : g.F_in;
     if constexpr (sizeof(T) == 4)
-        if (narrow_rows(K, N)) return launch_narrow_rows(MODE == kInput, g, s);
+        if (narrow_rows(g.m, K, N)) return launch_narrow_rows(MODE == kInput, g, s);
     if (direct && few_rows(sizeof(T) == 4, g.m, g.G, N))
         return launch_few(sizeof(T) == 4 ? EPP_FLOAT32 : std::is_same_v<T, __bf16> ? EPP_BFLOAT16 : EPP_FLOAT16, MODE == kInput, g, s);
     if constexpr (sizeof(T) == 2)
@@ -761,7 +761,7 @@ int grouped_rows(int mode, int type, const epp_rows_t* in, const void* W, const 
 // How the weight gradient cuts its entries: chunks of `per` entries of a group, at most `count` of them; per = 0: whole groups.
 struct Chunks { int64_t per, count; };
 Chunks chunking(bool fp32, int64_t m, int G, int F_in, int F_out) {
-    if (fp32 && narrow_weight(F_in, F_out)) {
+    if (fp32 && narrow_weight(m, F_in, F_out)) {
         const int64_t per = narrow_weight_chunk(m);
         return {per, std::max<int64_t>(most_tiles(m, G, per), 1)};
     }
@@ -822,7 +822,7 @@ int launch_sum(const GroupedArgs& g, int64_t chunks, TO* grad_W, hipStream_t s) 
 template <class T, class TO>
 int launch_weight(GroupedArgs g, const Chunks& c, bool direct, TO* grad_W, hipStream_t s) {
     if constexpr (sizeof(T) == 4)
-        if (narrow_weight(g.F_in, g.F_out)) {
+        if (narrow_weight(g.m, g.F_in, g.F_out)) {
             EPP_TRY(launch_narrow_weight(g, c.count, s));
             return launch_sum<TO>(g, c.count, grad_W, s);
         }

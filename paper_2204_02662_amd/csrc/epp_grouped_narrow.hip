@@ -1,4 +1,4 @@
-// Grouped products of narrow fp32 matrices (widths of up to 128): what the layers of a graph network are, with many entries.
+// Grouped products of narrow fp32 matrices (widths of up to 128) with many entries: what the layers of a graph network are.
 // They are bound by memory: 2 F_in F_out operations on 4 (F_in + F_out) bytes of an entry.
 //
 // Product and input gradient: a workgroup holds a group's weights in LDS and goes through up to 1,024 of its entries, 32 to a
@@ -19,7 +19,6 @@ namespace {
 
 constexpr int kMost = 128;       // width
 constexpr int kWaves = 8, kUnit = 32 * kWaves, kEntries = 4 * kUnit;  // product, input gradient: entries of a workgroup, at most
-constexpr int64_t kSplitMost = 16384;
 constexpr int kListed = 1024;    // weight gradient: entries whose rows are looked up at a time
 
 __device__ __attribute__((aligned(128))) float g_zeros[kMost] = {};
@@ -32,17 +31,15 @@ __device__ __forceinline__ void in_order() {
     __builtin_amdgcn_wave_barrier();
 }
 
-// K <= 32 P, N <= 32 NB.  SPLIT: a wavefront forms 32 columns, not all of them (few entries: there are more wavefronts than 32s of entries).
-template <int P, int NB, bool SPLIT>
+// K <= 32 P, N <= 32 NB.
+template <int P, int NB>
 __global__ __launch_bounds__(64 * kWaves) void k_narrow_rows(GroupedArgs g, int input, int units) {
-    constexpr int kOwn = SPLIT ? 1 : NB, kGroups = kWaves / (NB / kOwn), kRound = 32 * kGroups;  // blocks of a wavefront, 32s of entries at a time
     constexpr int kThreads = 64 * kWaves, kLd = 32 * P + 4;  // (16 lanes that read 16 bytes of neighbouring columns use all 64 banks)
     __shared__ __attribute__((aligned(16))) float Wl[32 * NB][kLd];  // [column][k]
     __shared__ __attribute__((aligned(128))) float turn[kWaves][32 * 32];
     __shared__ int32_t in_rows[kEntries], out_rows[kEntries];
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5;
-    const int K = input ? g.F_out : g.F_in, N = input ? g.F_in : g.F_out, per = kRound * units;
-    const int block0 = SPLIT ? w % NB : 0, wu = SPLIT ? w / NB : w;  // first block of this wavefront, and which 32 entries
+    const int K = input ? g.F_out : g.F_in, N = input ? g.F_in : g.F_out, per = kUnit * units;
     int64_t total;
     const Span s = find_group(g.offsets, g.G, g.m, per, blockIdx.x, &total);
     if (s.g < 0) return;
@@ -76,12 +73,12 @@ __global__ __launch_bounds__(64 * kWaves) void k_narrow_rows(GroupedArgs g, int 
     const int line = lane >> 3, piece = lane & 7, row = lane & 31;
     auto by_lines = [&](int i) { return reinterpret_cast<floatx4*>(mine + (line + 8 * i) * 32 + ((piece ^ (((line + 8 * i) >> 1) & 7)) * 4)); };
     auto by_columns = [&](int q) { return reinterpret_cast<floatx4*>(mine + row * 32 + (((2 * q + half) ^ ((row >> 1) & 7)) * 4)); };
-    const int rounds = wu < kGroups ? (count - 32 * wu + kRound - 1) / kRound : 0;  // of this wavefront
+    const int rounds = (count - 32 * w + kUnit - 1) / kUnit;  // of this wavefront
     // Numbers 32 p + 4 piece .. of the entries of unit u; zeros behind the last number, and for an entry without a row.
     auto load = [&](int u, floatx4 (&v)[P][4]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int32_t r = u < rounds ? in_rows[32 * wu + kRound * u + line + 8 * i] : -1;
+            const int32_t r = u < rounds ? in_rows[32 * w + kUnit * u + line + 8 * i] : -1;
             const float* p = r < 0 ? g_zeros : reinterpret_cast<const float*>(g.a.data + (int64_t)r * g.a.ld);
 #pragma unroll
             for (int q = 0; q < P; ++q) {
@@ -96,7 +93,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_narrow_rows(GroupedArgs g, int 
         }
     };
     auto multiply = [&](int u, floatx4 (&v)[P][4]) {
-        floatx16 acc[kOwn] = {};
+        floatx16 acc[NB] = {};
 #pragma unroll
         for (int q = 0; q < P; ++q) {
             if (32 * q >= K) continue;
@@ -117,23 +114,23 @@ __global__ __launch_bounds__(64 * kWaves) void k_narrow_rows(GroupedArgs g, int 
             for (int c = 0; c < 4; ++c) {
                 if (32 * q + 8 * c >= K) continue;
 #pragma unroll
-                for (int b = 0; b < kOwn; ++b) {
-                    const floatx4 y = *reinterpret_cast<const floatx4*>(&Wl[32 * (block0 + b) + row][32 * q + 8 * c + 4 * half]);
+                for (int b = 0; b < NB; ++b) {
+                    const floatx4 y = *reinterpret_cast<const floatx4*>(&Wl[32 * b + row][32 * q + 8 * c + 4 * half]);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) acc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(y[j], x[c][j], acc[b], 0, 0, 0);
                 }
             }
         }
 #pragma unroll
-        for (int b = 0; b < kOwn; ++b) {
+        for (int b = 0; b < NB; ++b) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) *by_columns(q) = floatx4{acc[b][4 * q], acc[b][4 * q + 1], acc[b][4 * q + 2], acc[b][4 * q + 3]};
             in_order();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int32_t r = out_rows[32 * wu + kRound * u + line + 8 * i];
+                const int32_t r = out_rows[32 * w + kUnit * u + line + 8 * i];
                 const floatx4 x = *by_lines(i);
-                const int c = 32 * (block0 + b) + 4 * piece;
+                const int c = 32 * b + 4 * piece;
                 if (r < 0 || c >= N) continue;
                 const float y[4] = {x[0], x[1], x[2], x[3]};
                 store4<float>(const_cast<char*>(g.out.data) + (int64_t)r * g.out.ld, c, y, N - c);
@@ -246,23 +243,15 @@ __global__ __launch_bounds__(256) void k_narrow_weight(GroupedArgs g) {
     }
 }
 
-template <int P, int NB, bool SPLIT>
-int launch_rows_of(bool input, const GroupedArgs& g, hipStream_t s) {
-    constexpr int kRound = SPLIT ? 32 * (kWaves / NB) : kUnit;
-    // as many entries to a workgroup as leave two of them to a compute unit
-    int units = kEntries / kUnit;
-    while (units > 1 && g.m < (int64_t)units * kRound * 2 * kUnits) units /= 2;
-    const int64_t per = kRound * units, blocks = (g.m + std::min<int64_t>(g.G, g.m) * (per - 1)) / per;
-    hipLaunchKernelGGL((k_narrow_rows<P, NB, SPLIT>), dim3((unsigned)blocks), dim3(64 * kWaves), 0, s, g, input ? 1 : 0, units);
-    EPP_HIP_TRY(hipGetLastError());
-    return EPP_OK;
-}
-
 template <int P, int NB>
 int launch_rows(bool input, const GroupedArgs& g, hipStream_t s) {
-    if constexpr (NB > 1)
-        if (g.m <= kSplitMost) return launch_rows_of<P, NB, true>(input, g, s);
-    return launch_rows_of<P, NB, false>(input, g, s);
+    // as many entries to a workgroup as leave two of them to a compute unit
+    int units = kEntries / kUnit;
+    while (units > 1 && g.m < (int64_t)units * kUnit * 2 * kUnits) units /= 2;
+    const int64_t per = kUnit * units, blocks = (g.m + std::min<int64_t>(g.G, g.m) * (per - 1)) / per;
+    hipLaunchKernelGGL((k_narrow_rows<P, NB>), dim3((unsigned)blocks), dim3(64 * kWaves), 0, s, g, input ? 1 : 0, units);
+    EPP_HIP_TRY(hipGetLastError());
+    return EPP_OK;
 }
 
 template <int P>
@@ -283,7 +272,12 @@ int launch_weight(const GroupedArgs& g, int64_t chunks, hipStream_t s) {
 
 }  // namespace
 
-bool epp_grouped::narrow_rows(int K, int N) { return K <= kMost && N <= kMost; }
+// Where these are faster than tiles of 64 x 64.  Four groups, rows named by lists, us, tiles / these: 64,000 entries, 16 x 41 10.6 / 9.1, its
+// gradient 12.0 / 8.8, 64 x 64 12.9 / 13.2; 250,000, 128 x 16 51 / 53, its gradient 53 / 37, 64 x 64 38 / 45; 1,000,000, 16 x 41 140 / 99,
+// 64 x 64 175 / 146, 128 x 128 419 / 377; 16,000, 16 x 41 6.5 / 6.6.
+bool epp_grouped::narrow_rows(int64_t m, int K, int N) {
+    return std::max(K, N) <= kMost && m >= (std::min(K, N) <= 32 ? 49152 : 1 << 19);
+}
 
 int epp_grouped::launch_narrow_rows(bool input, const GroupedArgs& g, hipStream_t s) {
     const int K = input ? g.F_out : g.F_in, N = input ? g.F_in : g.F_out;
@@ -293,7 +287,10 @@ int epp_grouped::launch_narrow_rows(bool input, const GroupedArgs& g, hipStream_
     return launch_rows_n<4>(N, input, g, s);
 }
 
-bool epp_grouped::narrow_weight(int F_in, int F_out) { return F_in <= kMost && F_out <= kMost; }
+// .. 64,000, 16 x 41 17.9 / 15.6; 1,000,000, 128 x 16 193 / 161; but 1,000,000, 64 x 47 133 / 151.
+bool epp_grouped::narrow_weight(int64_t m, int F_in, int F_out) {
+    return std::max(F_in, F_out) <= kMost && std::min(F_in, F_out) <= 32 && m >= 49152;
+}
 
 int64_t epp_grouped::narrow_weight_chunk(int64_t m) {
     // four workgroups to a compute unit, and no chunk that takes less time than its partial sums
@@ -302,5 +299,5 @@ int64_t epp_grouped::narrow_weight_chunk(int64_t m) {
 
 int epp_grouped::launch_narrow_weight(const GroupedArgs& g, int64_t chunks, hipStream_t s) {
     if (g.F_in <= 32) return g.F_out <= 32 ? launch_weight<1, 1>(g, chunks, s) : launch_weight<1, 2>(g, chunks, s);
-    return g.F_out <= 32 ? launch_weight<2, 1>(g, chunks, s) : launch_weight<2, 2>(g, chunks, s);
+    return launch_weight<2, 1>(g, chunks, s);
 }

@@ -121,16 +121,16 @@ def test_few_rows(m, G, Fi, Fo, dtype):
 @pytest.mark.parametrize("Fo", [2, 16, 32, 35, 56, 64, 66, 96, 100, 128])
 def test_narrow_floats(Fi, Fo):
     """Widths of up to 128, at the edges of the blocks of 32 and of the pieces of 16 bytes; few entries and many."""
-    for sizes in ([70, 0, 50, 1], [9_000, 31, 8_001, 700]):
+    for sizes in ([70, 0, 50, 1], [40_000, 31, 9_001, 700], [500_000, 24_300])[:2 if Fi > 40 or Fo in (2, 35, 66) else 3]:
         run_rows(sizes, Fi, Fo, torch.float32, False, Fi)
         run_rows(sizes, Fi, Fo, torch.float32, True, Fo)
         m, offsets = sum(sizes), offsets_of(sizes)
         x, d = randn(m, Fi, seed=13), randn(m, Fo, seed=14)
-        ws = torch.empty(epp.epp_grouped_weight_gradient_workspace(m, 4, Fi, Fo), dtype=torch.uint8, device=dev())
-        got = torch.empty(4, Fi, Fo, device=dev())
+        ws = torch.empty(epp.epp_grouped_weight_gradient_workspace(m, len(sizes), Fi, Fo), dtype=torch.uint8, device=dev())
+        got = torch.empty(len(sizes), Fi, Fo, device=dev())
         epp.epp_grouped_weight_gradient(x, d, offsets, got, ws)
         want, size, terms = weight_gradient(x, d, offsets, m)
-        assert_sums(got, want, size, terms + 520)
+        assert_sums(got, want, size, terms + 1_100)  # (up to 1,024 chunks)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
