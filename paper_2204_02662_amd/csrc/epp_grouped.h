@@ -103,6 +103,56 @@ __device__ __forceinline__ void load_to_lds(const char* base, unsigned off, unsi
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
 }
 
+// Between a wavefront's own writes to LDS and reads by other lanes of it, both ways: LDS serves them in order, and the compiler keeps it.
+__device__ __forceinline__ void in_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Pieces through registers.  One that the line's end cuts short is loaded so that it ends there, and shifted into place when it is put into
+// LDS: a load under a condition would be waited for where it stands.  Lines shorter than a piece are loaded element by element.
+typedef unsigned int any_uintx4 __attribute__((ext_vector_type(4), aligned(2)));
+
+template <class T>
+__device__ __forceinline__ uintx4 load_short(const char* p, int valid) {
+    constexpr int E = 16 / (int)sizeof(T);
+    uintx4 v = {0, 0, 0, 0};
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e < valid) v[e] = reinterpret_cast<const unsigned int*>(p)[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e < valid) v[e / 2] |= (unsigned int)reinterpret_cast<const unsigned short*>(p)[e] << (16 * (e % 2));
+    }
+    return v;
+}
+// The piece at p, of which `valid` elements are inside its line; zeros for none of them.
+template <class T>
+__device__ __forceinline__ uintx4 load_piece(const char* p, int valid, bool short_line, const char* zeros) {
+    constexpr int E = 16 / (int)sizeof(T);
+    if (short_line) return load_short<T>(p, valid);
+    return *reinterpret_cast<const any_uintx4*>(valid <= 0 ? zeros : valid >= E ? p : p - (E - valid) * (int)sizeof(T));
+}
+__device__ __forceinline__ uintx4 shifted(uintx4 v, int bits) {  // to lower addresses, zeros behind
+    unsigned long long lo = (unsigned long long)v[1] << 32 | v[0], hi = (unsigned long long)v[3] << 32 | v[2];
+    if (bits >= 64) {
+        lo = hi;
+        hi = 0;
+    }
+    const int s = bits & 63;
+    lo = s ? lo >> s | hi << (64 - s) : lo;
+    hi >>= s;
+    return uintx4{(unsigned int)lo, (unsigned int)(lo >> 32), (unsigned int)hi, (unsigned int)(hi >> 32)};
+}
+// What a piece of `valid` elements is to be shifted by.
+template <class T>
+__device__ __forceinline__ int shift_of(int valid, bool short_line) {
+    constexpr int E = 16 / (int)sizeof(T);
+    return valid > 0 && valid < E && !short_line ? (E - valid) * 8 * (int)sizeof(T) : 0;
+}
+
 // Four neighbouring results of a row; `valid` of them exist.  (A store needs no alignment beyond the element's.)
 template <class T>
 __device__ __forceinline__ void store4(char* row, int col, const float (&x)[4], int valid) {
@@ -117,9 +167,9 @@ __device__ __forceinline__ void store4(char* row, int col, const float (&x)[4], 
     }
 }
 
-// Kernels for few rows to a group (csrc/epp_grouped_few.hip); operands as direct loads want them.
-bool few_rows(bool fp32, int64_t m, int G, int N);
-int launch_few(int type, bool input, const GroupedArgs& g, hipStream_t s);
+// Kernels for few rows to a group (csrc/epp_grouped_few.hip).
+bool few_rows(bool fp32, bool input, bool direct, int64_t m, int G, int K, int N);
+int launch_few(int type, bool input, bool direct, const GroupedArgs& g, hipStream_t s);
 
 // Kernels of their own for narrow fp32 matrices (csrc/epp_grouped_narrow.hip).
 bool narrow_rows(int64_t m, int K, int N);  // of contraction K onto N columns

@@ -7,7 +7,7 @@
 // workgroups as m entries in G groups can need, and every one finds its tile by a scan of the offsets.
 //
 // A workgroup forms a TM x TN tile of the result from operand tiles of 128 bytes of the contraction (64 elements of 16
-// bits, 32 floats) in LDS, two of them: while the matrix cores work on one, the other fills.  An operand comes in one of
+// bits, 32 floats) in LDS, two of each or four: while the matrix cores work on one, the others fill.  An operand comes in one of
 // two ways:
 //   lines of K      the contraction is contiguous in memory (rows of X; W in the input gradient): a line of the tile is 128
 //                   bytes of one row
@@ -24,6 +24,11 @@
 // lines of 16 elements, and lane i gets the four of column i), floats one by one.  The first operand of the instruction is
 // the result's column, so that a lane holds four neighbouring columns of one row.
 // Sums are fp32; 16-bit results are rounded once, when they are written.
+//
+// What bounds them: large tiles of 16 bits the matrix cores together with what feeds them.  8,192 x 2,048 weights, 32 groups of 1,024
+// entries in bfloat16 run at 1,170 TFLOP/s (a library product of that size 1,290; these kernels without their loads of operands 1,430);
+// groups of uneven sizes lose another eighth to rows that are not there.  Floats: 129 of the matrix cores' 157 TFLOP/s.  The weight gradient
+// writes more than the products do: 256 KB a tile of floats, which nothing else in the compute unit overlaps.
 
 #include "epp_grouped.h"
 
@@ -65,49 +70,6 @@ template <int ALLOWED>
 __device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(ALLOWED) : "memory"); }
 
 __device__ __forceinline__ const char* zeros() { return reinterpret_cast<const char*>(g_zeros); }
-// Pieces through registers.  One that the line's end cuts short is loaded so that it ends there, and shifted into place when it is put into
-// LDS: a load under a condition would be waited for where it stands.  Lines shorter than a piece are loaded element by element.
-typedef unsigned int any_uintx4 __attribute__((ext_vector_type(4), aligned(2)));
-
-template <class T>
-__device__ __forceinline__ uintx4 load_short(const char* p, int valid) {
-    constexpr int E = 16 / (int)sizeof(T);
-    uintx4 v = {0, 0, 0, 0};
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (e < valid) v[e] = reinterpret_cast<const unsigned int*>(p)[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (e < valid) v[e / 2] |= (unsigned int)reinterpret_cast<const unsigned short*>(p)[e] << (16 * (e % 2));
-    }
-    return v;
-}
-// The piece at p, of which `valid` elements are inside its line; zeros for none of them.
-template <class T>
-__device__ __forceinline__ uintx4 load_piece(const char* p, int valid, bool short_line) {
-    constexpr int E = 16 / (int)sizeof(T);
-    if (short_line) return load_short<T>(p, valid);
-    return *reinterpret_cast<const any_uintx4*>(valid <= 0 ? zeros() : valid >= E ? p : p - (E - valid) * (int)sizeof(T));
-}
-__device__ __forceinline__ uintx4 shifted(uintx4 v, int bits) {  // to lower addresses, zeros behind
-    unsigned long long lo = (unsigned long long)v[1] << 32 | v[0], hi = (unsigned long long)v[3] << 32 | v[2];
-    if (bits >= 64) {
-        lo = hi;
-        hi = 0;
-    }
-    const int s = bits & 63;
-    lo = s ? lo >> s | hi << (64 - s) : lo;
-    hi >>= s;
-    return uintx4{(unsigned int)lo, (unsigned int)(lo >> 32), (unsigned int)hi, (unsigned int)(hi >> 32)};
-}
-// What a piece of `valid` elements is to be shifted by.
-template <class T>
-__device__ __forceinline__ int shift_of(int valid, bool short_line) {
-    constexpr int E = 16 / (int)sizeof(T);
-    return valid > 0 && valid < E && !short_line ? (E - valid) * 8 * (int)sizeof(T) : 0;
-}
 
 // Lines of K: TD rows, whose places are set once.  DIRECT: what stands in a line without a row is somebody's numbers (the result's row
 // is not written, or written as zeros); behind the contraction's end there are zeros.
@@ -147,7 +109,7 @@ struct LinesOfK {
             if (FULL) load_to_lds(base, off[i], at);
             else load_to_lds(k < K ? base + off[i] : zeros(), at);
         } else {
-            held[i] = load_piece<T>(p[i] + (int64_t)k * (int64_t)sizeof(T), p[i] ? K - k : 0, K < E);
+            held[i] = load_piece<T>(p[i] + (int64_t)k * (int64_t)sizeof(T), p[i] ? K - k : 0, K < E, zeros());
             shift = shift_of<T>(K - k, K < E);
             cut = !FULL;
         }
@@ -269,7 +231,7 @@ struct LinesOfWidth {
                 if (s.rows) r = row[i];
             }
             const bool no = e >= last || r < 0 || r >= s.n || c >= width;
-            held[i] = load_piece<T>(s.data + r * s.ld + (int64_t)c * (int64_t)sizeof(T), no ? 0 : width - c, width < E);
+            held[i] = load_piece<T>(s.data + r * s.ld + (int64_t)c * (int64_t)sizeof(T), no ? 0 : width - c, width < E, zeros());
         }
     }
     __device__ __forceinline__ void advance() {
@@ -355,8 +317,12 @@ __device__ __forceinline__ void form_tile(const GroupedArgs& g, const Place& at,
     }
 
     // Two sets of operand pieces in registers: while the matrix cores work on one, the other is read.  The wavefronts meet when all have
-    // read the last pieces of a tile, before they work on them: the tile's place is then free for the next but one, whose loads are issued
-    // between the last products, and the first pieces of the next arrive behind them.
+    // read the last pieces of a tile, before they work on them: the tile's place is then free for another, whose loads are issued at once
+    // (in between the last products instead, and thus later, they took 656 instead of 593 us for 32,768 entries, 32 groups, 4,096 x 2,048), and
+    // the first pieces of the next arrive behind the last products.
+    // kAcross: 32 lanes hold neighbouring columns, and write 128 bytes of a row; else a lane holds four neighbouring columns.  (Where writing
+    // floats is most of the work: 256 entries of 16 bits, 64 groups, 1,777 x 2,048, 201 / 171 us; floats from floats, whose tiles are small, 266 / 282.)
+    constexpr bool kAcross = MODE == kWeight && sizeof(T) == 2 && sizeof(TO) == 4;
     floatx16 acc[BM][BN] = {};
     uintx4 x[2][BM], y[2][BN];
     auto read = [&](const char* tile, int s, int set) {
@@ -366,12 +332,11 @@ __device__ __forceinline__ void form_tile(const GroupedArgs& g, const Place& at,
         for (int i = 0; i < BM; ++i) x[set][i] = A::piece(tile, 32 * (BM * wm + i), s);
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto multiply_block = [&](int set, int i, int j) { acc[i][j] = multiply<T>(y[set][j], x[set][i], acc[i][j]); };
     auto work = [&](int set) {
 #pragma unroll
         for (int i = 0; i < BM; ++i)
 #pragma unroll
-            for (int j = 0; j < BN; ++j) multiply_block(set, i, j);
+            for (int j = 0; j < BN; ++j) acc[i][j] = kAcross ? multiply<T>(x[set][i], y[set][j], acc[i][j]) : multiply<T>(y[set][j], x[set][i], acc[i][j]);
         __builtin_amdgcn_sched_barrier(0);
     };
     auto put = [&](char* tile) {
@@ -444,6 +409,21 @@ __device__ __forceinline__ void form_tile(const GroupedArgs& g, const Place& at,
     if (m0 + 32 * BM * wm < m_end) contract(Yes{});
     else contract(No{});
 
+    if constexpr (kAcross) {
+#pragma unroll
+        for (int i = 0; i < BM; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int64_t r = m0 + 32 * (BM * wm + i) + 8 * (e / 4) + 4 * (lane >> 5) + e % 4;
+                float* row = reinterpret_cast<float*>(at.out) + r * g.F_out;
+#pragma unroll
+                for (int j = 0; j < BN; ++j) {
+                    const int c = n0 + 32 * (BN * wn + j) + (lane & 31);
+                    if (r < m_end && c < N) row[c] = acc[i][j][e];
+                }
+            }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < BM; ++i) {
         const int64_t r = m0 + 32 * (BM * wm + i) + (lane & 31);
@@ -706,8 +686,8 @@ int launch_rows(const GroupedArgs& g, bool direct, hipStream_t s) {
     const int N = MODE == kInput ? g.F_in : g.F_out, K = MODE == kInput ? g.F_out : g.F_in;
     if constexpr (sizeof(T) == 4)
         if (narrow_rows(g.m, K, N)) return launch_narrow_rows(MODE == kInput, g, s);
-    if (direct && few_rows(sizeof(T) == 4, g.m, g.G, N))
-        return launch_few(sizeof(T) == 4 ? EPP_FLOAT32 : std::is_same_v<T, __bf16> ? EPP_BFLOAT16 : EPP_FLOAT16, MODE == kInput, g, s);
+    if (few_rows(sizeof(T) == 4, MODE == kInput, direct, g.m, g.G, K, N))
+        return launch_few(sizeof(T) == 4 ? EPP_FLOAT32 : std::is_same_v<T, __bf16> ? EPP_BFLOAT16 : EPP_FLOAT16, MODE == kInput, direct, g, s);
     if constexpr (sizeof(T) == 2)
         if (direct && large_tiles(g.m / 256 + g.G / 2, N)) return launch_rows_of<T, MODE, 2, 4, 4, 2, true, true>(g, s);
     if (sizeof(T) == 4 || small_tiles((g.m / 128 + g.G / 2) * ((N + 127) / 128))) {

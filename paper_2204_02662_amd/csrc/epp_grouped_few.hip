@@ -4,7 +4,7 @@
 // its part of the weights (and of the rows) from memory into a ring of its own in LDS, without waiting for the others, and they add up
 // their sums at the end.  Narrow tiles (32 or 64 columns) make enough workgroups for the chip even where only one or two groups have rows.
 // Loads go to LDS directly, kDepth steps ahead; behind the last step the ring is filled with zeros, so that the number of loads on
-// their way, which is what a wavefront waits by, is always the same.
+// their way, which is what a wavefront waits by, is always the same.  Rows that are no multiples of 16 bytes come through registers.
 //
 // Matrix instructions of 16 x 16: lane l supplies column (row) l % 16 and the contraction's piece of 16 bytes l / 16 of a step: one
 // instruction of 16 bits, four of floats.  As in the larger tiles, a piece's place in its line of LDS is permuted by the line's number, so that
@@ -38,14 +38,16 @@ __device__ __forceinline__ floatx4 multiply16(uintx4 a, uintx4 b, floatx4 c) {
 __device__ __forceinline__ const char* zeros() { return reinterpret_cast<const char*>(g_zeros); }
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
-template <class T, int MODE, int R, int TN>
+template <class T, int MODE, int R, int TN, bool DIRECT>
 __global__ __launch_bounds__(kThreads) void k_grouped_few(GroupedArgs g) {
     constexpr int size = (int)sizeof(T), E = 16 / size, KS = kStep / size, TM = 16 * R;
     constexpr int kX = TM * kStep, kW = TN * kStep, kStage = kX + kW, kLoads = kStage / 1024;
-    constexpr int kDepth = kStage * 4 <= 20480 ? 4 : 3;                // steps in the ring
+    constexpr int kDepth = !DIRECT ? 1 : kStage * 4 <= 20480 ? 4 : 3;  // steps in the ring
+    constexpr int kAhead = kLoads <= 5 ? 4 : 3;                        // not DIRECT: steps on their way to registers
+    constexpr int kBlocks = R * (TN / 16), kSums = kBlocks * 1024;     // bytes of a wavefront's results
     constexpr int kWide = TN * size, kPieces = kWide / 16;             // product: a line of the weights, one step of the contraction
     static_assert(kX % 1024 == 0 && kW % 1024 == 0 && kLoads * (kDepth - 1) < 64, "ring");
-    __shared__ __attribute__((aligned(128))) char ring[kWaves][kDepth * kStage];
+    __shared__ __attribute__((aligned(128))) char ring[kWaves][kDepth * kStage > kSums ? kDepth * kStage : kSums];
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), q = lane >> 4, l16 = lane & 15;
     const int N = MODE == kInput ? g.F_in : g.F_out, K = MODE == kInput ? g.F_out : g.F_in, nt = (N + TN - 1) / TN;
     // Workgroups b, b + 8, .. run on one XCD: it gets neighbouring columns, whose lines its L2 holds.
@@ -77,17 +79,19 @@ __global__ __launch_bounds__(kThreads) void k_grouped_few(GroupedArgs g) {
         else return TN == 64 ? ((line >> 1) & 1) | (((line >> 3) & 1) << 1) : (line >> 3) & 1;
     };
     const char* pw[kWLoads];
-    int kw[kWLoads];
+    int kw[kWLoads], left[kWLoads];  // (product: columns from a piece's first to the end)
 #pragma unroll
     for (int i = 0; i < kWLoads; ++i) {
         if constexpr (MODE == kInput) {
             const int n = 16 * i + (lane >> 2);
             kw[i] = ((lane & 3) ^ ((n >> 2) & 3)) * E;
             pw[i] = W + (int64_t)min(n0 + n, N - 1) * ldw;  // (columns behind the width: somebody's numbers, for a result that is not written)
+            left[i] = 0;
         } else {
             const int line = (64 * i + lane) / kPieces, c = n0 + (((64 * i + lane) % kPieces) ^ (turn(line) << 1)) * E;
             kw[i] = line;
             pw[i] = W + (int64_t)(c < N ? c : 0) * size;
+            left[i] = c < N ? N - c : N;
         }
     }
     const unsigned base = __builtin_amdgcn_readfirstlane(lds_address(ring[w]));
@@ -104,13 +108,7 @@ __global__ __launch_bounds__(kThreads) void k_grouped_few(GroupedArgs g) {
         }
     };
     floatx4 acc[R][TN / 16] = {};
-    for (int i = 0; i < kDepth - 1; ++i) fetch(first + i, i);
-    int slot = 0;
-    for (int st = first; st < last; ++st) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        fetch(st + kDepth - 1, slot == 0 ? kDepth - 1 : slot - 1);
-        wait_loads<kLoads * (kDepth - 1)>();
-        const char* tile = ring[w] + slot * kStage;
+    auto work = [&](const char* tile) {
         uintx4 x[R], y[TN / 16];
 #pragma unroll
         for (int i = 0; i < R; ++i) x[i] = *reinterpret_cast<const uintx4*>(tile + (16 * i + l16) * kStep + ((q ^ ((l16 >> 2) & 3)) * 16));
@@ -137,12 +135,61 @@ __global__ __launch_bounds__(kThreads) void k_grouped_few(GroupedArgs g) {
         for (int i = 0; i < R; ++i)
 #pragma unroll
             for (int j = 0; j < TN / 16; ++j) acc[i][j] = multiply16<T>(y[j], x[i], acc[i][j]);
-        slot = slot + 1 == kDepth ? 0 : slot + 1;
+    };
+    if constexpr (DIRECT) {
+        for (int i = 0; i < kDepth - 1; ++i) fetch(first + i, i);
+        int slot = 0;
+        for (int st = first; st < last; ++st) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            fetch(st + kDepth - 1, slot == 0 ? kDepth - 1 : slot - 1);
+            wait_loads<kLoads * (kDepth - 1)>();
+            work(ring[w] + slot * kStage);
+            slot = slot + 1 == kDepth ? 0 : slot + 1;
+        }
+    } else {
+        // Pieces of any alignment: through registers, kAhead steps on their way.
+        uintx4 held[kAhead][kLoads];
+        auto load = [&](int st, uintx4 (&v)[kLoads]) {
+            const int k0 = st < last ? st * KS : K;  // (behind the last step: zeros)
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                v[i] = load_piece<T>(px[i] + (int64_t)(k0 + kx[i]) * size, px[i] ? K - (k0 + kx[i]) : 0, false, zeros());
+#pragma unroll
+            for (int i = 0; i < kWLoads; ++i) {
+                if constexpr (MODE == kInput) v[R + i] = load_piece<T>(pw[i] + (int64_t)(k0 + kw[i]) * size, K - (k0 + kw[i]), false, zeros());
+                else v[R + i] = load_piece<T>(pw[i] + (int64_t)(k0 + kw[i]) * ldw, k0 + kw[i] < K ? left[i] : 0, false, zeros());
+            }
+        };
+        auto put = [&](int st, const uintx4 (&v)[kLoads]) {
+            const bool end = (st + 1) * KS > K, edge = n0 + TN > N;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                uintx4 x = v[i];
+                if (i < R || MODE == kInput) {
+                    if (end) x = shifted(x, shift_of<T>(K - (st * KS + (i < R ? kx[i < R ? i : 0] : kw[i < R ? 0 : i - R])), false));
+                } else if (edge) {
+                    x = shifted(x, shift_of<T>(left[i < R ? 0 : i - R], false));
+                }
+                *reinterpret_cast<uintx4*>(ring[w] + i * 1024 + lane * 16) = x;
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) load(first + i, held[i]);
+        for (int st = first; st < last; st += kAhead) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (st + i < last) {
+                    in_order();
+                    put(st + i, held[i]);
+                    in_order();
+                    load(st + i + kAhead, held[i]);
+                    work(ring[w]);
+                }
+            }
+        }
     }
     // The wavefronts' sums, added in order: lane l of a block has columns 4 (l / 16) .. + 3 of row l % 16.
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    constexpr int kBlocks = R * (TN / 16);
-    static_assert(kWaves * kBlocks * 64 * 16 <= (int)sizeof(ring), "sums");
     floatx4* sums = reinterpret_cast<floatx4*>(&ring[0][0]);
 #pragma unroll
     for (int i = 0; i < R; ++i)
@@ -161,50 +208,56 @@ __global__ __launch_bounds__(kThreads) void k_grouped_few(GroupedArgs g) {
     }
 }
 
-template <class T, int MODE, int R, int TN>
+template <class T, int MODE, int R, int TN, bool DIRECT>
 int launch_of(const GroupedArgs& g, hipStream_t s) {
     constexpr int TM = 16 * R;
     const int N = MODE == kInput ? g.F_in : g.F_out;
     const int64_t blocks = ((g.m + std::min<int64_t>(g.G, g.m) * (TM - 1)) / TM * ((N + TN - 1) / TN) + 7) / 8 * 8;
     if (blocks > 0x7FFFFFFF) { epp_set_error("%lld workgroups in one launch", (long long)blocks); return EPP_ERR_TOO_LARGE; }
-    hipLaunchKernelGGL((k_grouped_few<T, MODE, R, TN>), dim3((unsigned)blocks), dim3(kThreads), 0, s, g);
+    hipLaunchKernelGGL((k_grouped_few<T, MODE, R, TN, DIRECT>), dim3((unsigned)blocks), dim3(kThreads), 0, s, g);
     EPP_HIP_TRY(hipGetLastError());
     return EPP_OK;
 }
 
-template <class T, int MODE, int R>
+template <class T, int MODE, int R, bool DIRECT>
 int launch_columns(const GroupedArgs& g, hipStream_t s) {
     const int N = MODE == kInput ? g.F_in : g.F_out;
     const int64_t groups = std::min<int64_t>(g.G, g.m);
-    if (groups * ((N + 63) / 64) >= 2 * kUnits) return launch_of<T, MODE, R, 64>(g, s);
-    return launch_of<T, MODE, R, 32>(g, s);
+    if (groups * ((N + 63) / 64) >= 2 * kUnits) return launch_of<T, MODE, R, 64, DIRECT>(g, s);
+    return launch_of<T, MODE, R, 32, DIRECT>(g, s);
 }
 
 // Rows of a tile: as many as most groups have.  (Floats: never 64, which would mostly be products of rows that are not there: 128 entries in
 // 8 groups, 2,048 x 4,096, 84 us with 32 rows and 140 with 64.)
-template <class T, int MODE>
+template <class T, int MODE, bool DIRECT>
 int launch_mode(const GroupedArgs& g, hipStream_t s) {
-    if (g.m <= 8 * (int64_t)g.G) return launch_columns<T, MODE, 1>(g, s);
-    if (sizeof(T) == 4 || g.m <= 24 * (int64_t)g.G) return launch_columns<T, MODE, 2>(g, s);
-    return launch_columns<T, MODE, 4>(g, s);
+    if (g.m <= 8 * (int64_t)g.G) return launch_columns<T, MODE, 1, DIRECT>(g, s);
+    if (sizeof(T) == 4 || g.m <= 24 * (int64_t)g.G) return launch_columns<T, MODE, 2, DIRECT>(g, s);
+    if constexpr (sizeof(T) == 2) return launch_columns<T, MODE, 4, DIRECT>(g, s);
+    return EPP_ERR_INVALID_ARG;  // (not reached)
 }
 
 template <class T>
-int launch_type(bool input, const GroupedArgs& g, hipStream_t s) { return input ? launch_mode<T, kInput>(g, s) : launch_mode<T, kProduct>(g, s); }
+int launch_type(bool input, bool direct, const GroupedArgs& g, hipStream_t s) {
+    if (direct) return input ? launch_mode<T, kInput, true>(g, s) : launch_mode<T, kProduct, true>(g, s);
+    return input ? launch_mode<T, kInput, false>(g, s) : launch_mode<T, kProduct, false>(g, s);
+}
 
 }  // namespace
 
 // Fewer than 32 rows to a group on average, and 16 bits only where the larger tiles are not enough to fill the chip with loads.  Larger tiles
 // against these, us: bfloat16, 8 groups, 2 entries, 2,048 x 4,096 (64 tiles of 128 x 128) 22.2 / 9.2; 64, 4,096 x 1,024 (64) 38.5 / 23.0;
 // 256 of the same 39.1 / 31.4; but 64, 2,048 x 4,096 (256) 25.5 / 35.2 and 64 groups, 256, 2,048 x 4,096 201 / 198.  Floats: 8 groups, 16
-// entries, 4,096 x 1,024 250 / 27; 64 groups, 1,024, 2,048 x 4,096 980 / 604; 2,048 of the same 1,077 / 1,105.
-bool epp_grouped::few_rows(bool fp32, int64_t m, int G, int N) {
+// entries, 4,096 x 1,024 250 / 27; 64 groups, 1,024, 2,048 x 4,096 980 / 604; 2,048 of the same 1,077 / 1,105.  Rows of any alignment the same, but for
+// the input gradient of floats: 8 groups, 2 entries, 1,777 x 1,333 60 / 17; 64 groups, 256, 800 x 3,329 164 / 148, its gradient 161 / 207.
+bool epp_grouped::few_rows(bool fp32, bool input, bool direct, int64_t m, int G, int K, int N) {
+    if (std::min(K, N) < 8) return false;  // (rows shorter than a piece)
     if (m >= (fp32 ? 24 : 32) * (int64_t)G) return false;
-    return fp32 || std::min<int64_t>(G, m) * ((N + 127) / 128) < kUnits;
+    return (fp32 && (direct || !input)) || std::min<int64_t>(G, m) * ((N + 127) / 128) < kUnits;
 }
 
-int epp_grouped::launch_few(int type, bool input, const GroupedArgs& g, hipStream_t s) {
-    if (type == EPP_FLOAT32) return launch_type<float>(input, g, s);
-    if (type == EPP_BFLOAT16) return launch_type<__bf16>(input, g, s);
-    return launch_type<_Float16>(input, g, s);
+int epp_grouped::launch_few(int type, bool input, bool direct, const GroupedArgs& g, hipStream_t s) {
+    if (type == EPP_FLOAT32) return launch_type<float>(input, direct, g, s);
+    if (type == EPP_BFLOAT16) return launch_type<__bf16>(input, direct, g, s);
+    return launch_type<_Float16>(input, direct, g, s);
 }

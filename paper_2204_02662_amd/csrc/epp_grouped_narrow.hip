@@ -25,12 +25,6 @@ __device__ __attribute__((aligned(128))) float g_zeros[kMost] = {};
 
 typedef float any_floatx4 __attribute__((ext_vector_type(4), aligned(4)));
 
-// Between a wavefront's own writes to LDS and reads by other lanes of it, both ways: LDS serves them in order, and the compiler keeps it.
-__device__ __forceinline__ void in_order() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // K <= 32 P, N <= 32 NB.
 template <int P, int NB>
 __global__ __launch_bounds__(64 * kWaves) void k_narrow_rows(GroupedArgs g, int input, int units) {

@@ -108,7 +108,7 @@ def test_lists_strides_and_what_is_left(Fi, Fo, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("m,G,Fi,Fo", [(1, 8, 512, 768), (2, 8, 1000, 1016), (16, 16, 777, 520), (17, 3, 2048, 256), (64, 64, 520, 1024),
-                                       (200, 32, 640, 512)])
+                                       (200, 32, 640, 512), (1, 4, 1777, 1333), (30, 8, 8, 9), (60, 4, 9, 801), (90, 4, 801, 33), (100, 4, 130, 1021)])
 def test_few_rows(m, G, Fi, Fo, dtype):
     """A handful of rows to a group and wide matrices, as single tokens are served."""
     gen = torch.Generator("cpu").manual_seed(m)
