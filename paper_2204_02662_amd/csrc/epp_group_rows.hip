@@ -3,8 +3,9 @@
 //
 // Few entries: one workgroup counts, sums and places them.  Many: blocks of consecutive entries are counted, and then place their
 // entries; the counts of the blocks before are added up by every block itself where they are few, else by a wavefront per group in a
-// launch between.  A wavefront finds an entry's rank among its 64 by
-// ballots over the bits of the group's number; nothing depends on the order in which blocks or wavefronts run.
+// launch between.  A wavefront finds an entry's rank among its 64 by ballots over the bits of the group's number; nothing depends on the
+// order in which blocks or wavefronts run.  Few bytes, and bound by the steps that wait for each other: 1,000,000 entries of 8 groups, 8 MB,
+// take 13.7 us where a copy takes 1.6.
 // Group G stands for "no group": its entries come last.
 
 #include "epp_internal.h"
@@ -27,57 +28,67 @@ struct GroupRowsArgs {
     int32_t *counts, *totals;  // counts[group][block], totals[group] (NULL: counts are few, and not yet summed over the blocks)
 };
 
-// f(entry, row, group) for the entries [first, last) of the calling wavefront, 64 at a time, in order, with the numbers of kAhead times 64
-// entries on their way together (their rows first, then their groups).
-template <class F>
-__device__ __forceinline__ void for_entries(const GroupRowsArgs& a, int64_t first, int64_t last, F f) {
-    constexpr int kAhead = 8;
-    const int lane = threadIdx.x & 63;
-    for (int64_t i0 = first; i0 < last; i0 += 64 * kAhead) {
-        int32_t row[kAhead], group[kAhead];
+// Rows and groups of up to kAhead times 64 entries [first, last) (at least one), a lane's share: entry first + 64 j + lane.  All of their rows are on
+// their way together, and then all of their groups.
+constexpr int kAhead = kBlockEntries / kWaves / 64;
+struct Entries {
+    int32_t row[kAhead], group[kAhead];
+    __device__ __forceinline__ void load(const GroupRowsArgs& a, int64_t first, int64_t last) {
+        const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            const int64_t i = min(i0 + 64 * j + lane, last - 1);
+            const int64_t i = min(first + 64 * j + lane, last - 1);
             row[j] = a.rows ? a.rows[i] : (int32_t)i;
         }
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const bool there = row[j] >= 0 && row[j] < a.n;
-            group[j] = there ? a.group_of[row[j]] : -1;
-        }
+        for (int j = 0; j < kAhead; ++j) group[j] = row[j] >= 0 && row[j] < a.n ? a.group_of[row[j]] : -1;
+    }
+    // Adds the entries' groups to count[].
+    __device__ __forceinline__ void count(const GroupRowsArgs& a, int64_t first, int64_t last, int32_t* count) const {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (first + 64 * j + lane < last) atomicAdd(&count[group[j] >= 0 && group[j] < a.G ? group[j] : a.G], 1);
+    }
+    // Places the entries from next[] on, which is the calling wavefront's own.
+    __device__ __forceinline__ void place(const GroupRowsArgs& a, int64_t first, int64_t last, volatile int32_t* next) const {
+        const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
+            if (first + 64 * j >= last) break;
+            const bool have = first + 64 * j + lane < last;
             const int g = group[j] >= 0 && group[j] < a.G ? group[j] : a.G;
-            if (i0 + 64 * j < last) f(i0 + 64 * j + lane < last, row[j], g);
+            unsigned long long same = __ballot(have);
+            for (int b = 0; b < a.bits; ++b) {
+                const unsigned long long set = __ballot((g >> b) & 1);
+                same &= (g >> b) & 1 ? set : ~set;
+            }
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            if (have) {
+                const int32_t at = next[g];
+                __builtin_amdgcn_wave_barrier();
+                if (rank == 0) next[g] = at + __popcll(same);
+                __builtin_amdgcn_wave_barrier();
+                a.order[at + rank] = row[j];
+            }
         }
     }
-}
+};
 
-// Adds the group counts of entries [first, last) to count[], by the calling wavefront.
+// The same for any number of entries of the calling wavefront.
 __device__ __forceinline__ void count_entries(const GroupRowsArgs& a, int64_t first, int64_t last, int32_t* count) {
-    for_entries(a, first, last, [&](bool have, int32_t, int g) {
-        if (have) atomicAdd(&count[g], 1);
-    });
+    for (int64_t i = first; i < last; i += 64 * kAhead) {
+        Entries e;
+        e.load(a, i, last);
+        e.count(a, i, last, count);
+    }
 }
-
-// Places entries [first, last) from next[] on, by the calling wavefront, which owns next[].
 __device__ __forceinline__ void place_entries(const GroupRowsArgs& a, int64_t first, int64_t last, volatile int32_t* next) {
-    const int lane = threadIdx.x & 63;
-    for_entries(a, first, last, [&](bool have, int32_t row, int g) {
-        unsigned long long same = __ballot(have);
-        for (int b = 0; b < a.bits; ++b) {
-            const unsigned long long set = __ballot((g >> b) & 1);
-            same &= (g >> b) & 1 ? set : ~set;
-        }
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        if (have) {
-            const int32_t at = next[g];
-            __builtin_amdgcn_wave_barrier();
-            if (rank == 0) next[g] = at + __popcll(same);
-            __builtin_amdgcn_wave_barrier();
-            a.order[at + rank] = row;
-        }
-    });
+    for (int64_t i = first; i < last; i += 64 * kAhead) {
+        Entries e;
+        e.load(a, i, last);
+        e.place(a, i, last, next);
+    }
 }
 
 // Exclusive sums over `n` values, 64 at a time, by one wavefront.  Returns the sum of all.
@@ -155,6 +166,11 @@ __global__ __launch_bounds__(64 * kWaves) void k_group_place(GroupRowsArgs a) {
     extern __shared__ int32_t next[];  // [wavefront][group], and before that the groups' beginnings in the first row
     __shared__ int32_t before_here[kFewSums + 1];
     const int t = threadIdx.x, w = t >> 6, groups = a.G + 1;
+    const int64_t first = (int64_t)blockIdx.x * a.per, share = a.per / kWaves;
+    const int64_t mine = min(first + w * share, a.m), last = min(mine + share, a.m);
+    const bool once = a.per == kBlockEntries && mine < last;  // few enough entries to hold: they are looked up once, and while the counts are added up
+    Entries held;
+    if (once) held.load(a, mine, last);
     for (int i = groups + t; i < kWaves * groups; i += 64 * kWaves) next[i] = 0;
     if (a.totals) {
         for (int i = t; i < groups; i += 64 * kWaves) next[i] = a.totals[i];
@@ -185,9 +201,10 @@ __global__ __launch_bounds__(64 * kWaves) void k_group_place(GroupRowsArgs a) {
     if (blockIdx.x == 0)
         for (int g = t; g < groups; g += 64 * kWaves) a.offsets[g] = next[g];
     // next[x][g], x >= 1: what wavefronts before x have of group g, after the sums below
-    const int64_t first = (int64_t)blockIdx.x * a.per, share = a.per / kWaves;
-    const int64_t mine = min(first + w * share, a.m), last = min(mine + share, a.m);
-    if (w + 1 < kWaves) count_entries(a, mine, last, next + (w + 1) * groups);
+    if (w + 1 < kWaves) {
+        if (once) held.count(a, mine, last, next + (w + 1) * groups);
+        else count_entries(a, mine, last, next + (w + 1) * groups);
+    }
     __syncthreads();
     for (int g = t; g < groups; g += 64 * kWaves) {
         int32_t sum = next[g] + (a.totals ? a.counts[(int64_t)g * a.blocks + blockIdx.x] : before_here[g]);
@@ -199,7 +216,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_group_place(GroupRowsArgs a) {
         }
     }
     __syncthreads();
-    place_entries(a, mine, last, next + w * groups);
+    if (once) held.place(a, mine, last, next + w * groups);
+    else place_entries(a, mine, last, next + w * groups);
 }
 
 int check(int64_t m, int G) {
