@@ -336,7 +336,8 @@ typedef struct {
     void* data;          /* device, row-major                                                    */
     int64_t n;           /* rows, < 2^31                                                         */
     int64_t ld;          /* elements from row to row, at least the width                         */
-    const int32_t* rows; /* device, m; a row outside [0, n) counts as zeros and is never written */
+    const int32_t* rows; /* device, m; a row outside [0, n) counts as zeros and is never written
+                            (times a weight that is infinite or NaN: zero or NaN) */
 } epp_rows_t;
 
 /* Products of a layer with a weight matrix per group, entry i in group g:
@@ -353,7 +354,8 @@ typedef struct {
  *   grad_W     device, G x F_in x F_out of `type` or EPP_FLOAT32, overwritten (zeros for a group without entries)
  *   workspace  device, at least epp_grouped_weight_gradient_workspace(...) bytes, 16-byte aligned: partial sums over blocks of
  *              entries, which a second kernel adds in a fixed order
- * 1 <= G <= 2048, 1 <= F_in, F_out <= 65,536, 0 <= m < 2^31.  Outputs must not alias inputs (columns of one wider matrix are fine). */
+ * 1 <= G <= 2048, 1 <= F_in, F_out <= 65,536, 0 <= m < 2^31, and a result of fewer than 2^24 tiles (64 x 64 elements of fp32, 128 x 128
+ * of 16 bits, each group's own), else EPP_ERR_TOO_LARGE.  Outputs must not alias inputs (columns of one wider matrix are fine). */
 int epp_grouped_product(int type, const epp_rows_t* X, const void* W, const int32_t* offsets, int G, int64_t m, int F_in, int F_out,
                         const epp_rows_t* out, epp_stream_t stream);
 int epp_grouped_input_gradient(int type, const epp_rows_t* grad_out, const void* W, const int32_t* offsets, int G, int64_t m, int F_in,
@@ -382,7 +384,8 @@ typedef struct {
  *   norm       device, one float
  *   workspace  device, at least epp_gradient_norm_workspace(n) bytes, 16-byte aligned
  * What is written must not overlap with anything else: a gradient listed twice is refused by epp_clip_gradients (and counts twice in
- * epp_gradient_norm).  Enqueues only: one launch for the norm of up to 96 gradients, one to finish or to scale. */
+ * epp_gradient_norm).  Enqueues only: one launch for the norm of up to 96 gradients and one to
+ * finish or to scale, or a single one for gradients of few elements (about 32 times 1,024). */
 int64_t epp_gradient_norm_workspace(int n); /* bytes, < 0: error */
 int epp_gradient_norm(const epp_gradient_t* grads, int n, float* norm, void* workspace, int64_t workspace_bytes, epp_stream_t stream);
 int epp_clip_gradients(const epp_gradient_t* grads, int n, double max_norm, float* norm, void* workspace, int64_t workspace_bytes,

@@ -31,7 +31,8 @@ struct GroupedArgs {
     int64_t m;
     int G, F_in, F_out;
     int64_t per;        // weight gradient: entries to a chunk (0: whole groups)
-    float* part;        // .. and its partial sums
+    int64_t chunks;     // .. how many chunks there can be (offsets that descend name more of them)
+    float* part;        // .. and their partial sums
 };
 
 // ---------------------------------------------------------------- numbers

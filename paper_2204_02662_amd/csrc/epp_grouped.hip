@@ -553,8 +553,8 @@ __global__ __launch_bounds__(256) void k_grouped_sum(GroupedArgs g, TO* __restri
             count += __shfl_xor(count, d, 64);
         }
         if (lane == 0) {
-            span[0] = before;
-            span[1] = count;
+            span[0] = min(before, g.chunks);
+            span[1] = min(count, g.chunks - span[0]);
         }
     }
     __syncthreads();
@@ -646,6 +646,10 @@ bool overlaps_block(const epp_rows_t& x, int wx, int size, const void* p, int64_
     const uintptr_t bp = reinterpret_cast<uintptr_t>(p);
     return bx < bp + (uintptr_t)bytes && bp < ex;
 }
+bool overlaps_offsets(const int32_t* offsets, int G, const void* p, int64_t bytes) {
+    const uintptr_t o = reinterpret_cast<uintptr_t>(offsets), b = reinterpret_cast<uintptr_t>(p);
+    return o < b + (uintptr_t)bytes && b < o + 4 * ((uintptr_t)G + 1);
+}
 int aliased() { epp_set_error("matrices must not alias"); return EPP_ERR_INVALID_ARG; }
 
 bool aligned(const Side& s, int width_bytes) { return (reinterpret_cast<uintptr_t>(s.data) | (uintptr_t)s.ld | (uintptr_t)width_bytes) % 16 == 0; }
@@ -654,7 +658,12 @@ Side side(const epp_rows_t& x, int size) { return {static_cast<const char*>(x.da
 // Tiles of `tile` entries that m entries in G groups can make.
 int64_t most_tiles(int64_t m, int64_t G, int64_t tile) { return (m + std::min(G, m) * (tile - 1)) / tile; }
 
-int too_many(int64_t blocks) { epp_set_error("%lld workgroups in one launch", (long long)blocks); return EPP_ERR_TOO_LARGE; }
+// (a launch has fewer than 2^32 threads)
+int check_blocks(int64_t blocks, int threads) {
+    if (blocks * threads <= 0xFFFFFFFFll) return EPP_OK;
+    epp_set_error("%lld tiles of the result in one launch", (long long)blocks);
+    return EPP_ERR_TOO_LARGE;
+}
 
 template <class T, int MODE, int WM, int WN, int BM, int BN, bool DIRECT, bool QUARTERS, int STAGES = 2>
 int launch_rows_of(const GroupedArgs& g, hipStream_t s) {
@@ -662,7 +671,7 @@ int launch_rows_of(const GroupedArgs& g, hipStream_t s) {
     const int N = MODE == kInput ? g.F_in : g.F_out;
     int64_t blocks = most_tiles(g.m, g.G, TM) * ((N + TN - 1) / TN) + 16;
     if (QUARTERS) blocks += 3 * (kUnits / 2);
-    if (blocks > 0x7FFFFFFF) return too_many(blocks);
+    EPP_TRY(check_blocks(blocks, 64 * WM * WN));
     hipLaunchKernelGGL((k_grouped_rows<T, MODE, WM, WN, BM, BN, DIRECT, QUARTERS, STAGES>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, g);
     EPP_HIP_TRY(hipGetLastError());
     return EPP_OK;
@@ -763,7 +772,7 @@ template <class T, class TO, int WM, int WN, int BM, int BN, bool DIRECT, bool L
 int launch_weight_of(const GroupedArgs& g, int64_t chunks, hipStream_t s) {
     constexpr int TM = 32 * WM * BM, TN = 32 * WN * BN;
     const int64_t blocks = chunks * ((g.F_in + TM - 1) / TM) * ((g.F_out + TN - 1) / TN);
-    if (blocks > 0x7FFFFFFF) return too_many(blocks);
+    EPP_TRY(check_blocks(blocks, 64 * WM * WN));
     hipLaunchKernelGGL((k_grouped_weight<T, TO, WM, WN, BM, BN, DIRECT, LIST, STAGES>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, g);
     EPP_HIP_TRY(hipGetLastError());
     return EPP_OK;
@@ -857,7 +866,8 @@ extern "C" int epp_grouped_weight_gradient(int type, const epp_rows_t* X, const 
     if (overlaps_block(*X, F_in, size, grad_W, w_bytes) || overlaps_block(*grad_out, F_out, size, grad_W, w_bytes) ||
         overlaps_block(*X, F_in, size, workspace, need) || overlaps_block(*grad_out, F_out, size, workspace, need) ||
         (reinterpret_cast<uintptr_t>(workspace) < reinterpret_cast<uintptr_t>(grad_W) + (uintptr_t)w_bytes &&
-         reinterpret_cast<uintptr_t>(grad_W) < reinterpret_cast<uintptr_t>(workspace) + (uintptr_t)need))
+         reinterpret_cast<uintptr_t>(grad_W) < reinterpret_cast<uintptr_t>(workspace) + (uintptr_t)need) ||
+        overlaps_offsets(offsets, G, grad_W, w_bytes) || overlaps_offsets(offsets, G, workspace, need))
         return aliased();
     GroupedArgs g = {};
     g.a = side(*X, size);
@@ -869,6 +879,7 @@ extern "C" int epp_grouped_weight_gradient(int type, const epp_rows_t* X, const 
     g.F_out = F_out;
     const Chunks c = chunking(type == EPP_FLOAT32, m, G, F_in, F_out);
     g.per = c.per;
+    g.chunks = c.count;
     g.part = static_cast<float*>(workspace);
     const bool direct = aligned(g.a, F_in * size) && aligned(g.b, F_out * size) && std::max(g.a.ld, g.b.ld) < (1 << 26);
     hipStream_t s = (hipStream_t)stream;

@@ -213,7 +213,6 @@ int launch_of(const GroupedArgs& g, hipStream_t s) {
     constexpr int TM = 16 * R;
     const int N = MODE == kInput ? g.F_in : g.F_out;
     const int64_t blocks = ((g.m + std::min<int64_t>(g.G, g.m) * (TM - 1)) / TM * ((N + TN - 1) / TN) + 7) / 8 * 8;
-    if (blocks > 0x7FFFFFFF) { epp_set_error("%lld workgroups in one launch", (long long)blocks); return EPP_ERR_TOO_LARGE; }
     hipLaunchKernelGGL((k_grouped_few<T, MODE, R, TN, DIRECT>), dim3((unsigned)blocks), dim3(kThreads), 0, s, g);
     EPP_HIP_TRY(hipGetLastError());
     return EPP_OK;
@@ -245,7 +244,7 @@ int launch_type(bool input, bool direct, const GroupedArgs& g, hipStream_t s) {
 
 }  // namespace
 
-// Fewer than 32 rows to a group on average, and 16 bits only where the larger tiles are not enough to fill the chip with loads.  Larger tiles
+// Fewer than 32 rows to a group on average (so that no launch has 2^32 threads), and 16 bits only where the larger tiles are not enough to fill the chip with loads.  Larger tiles
 // against these, us: bfloat16, 8 groups, 2 entries, 2,048 x 4,096 (64 tiles of 128 x 128) 22.2 / 9.2; 64, 4,096 x 1,024 (64) 38.5 / 23.0;
 // 256 of the same 39.1 / 31.4; but 64, 2,048 x 4,096 (256) 25.5 / 35.2 and 64 groups, 256, 2,048 x 4,096 201 / 198.  Floats: 8 groups, 16
 // entries, 4,096 x 1,024 250 / 27; 64 groups, 1,024, 2,048 x 4,096 980 / 604; 2,048 of the same 1,077 / 1,105.  Rows of any alignment the same, but for

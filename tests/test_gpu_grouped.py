@@ -181,6 +181,21 @@ def test_offsets_that_are_not_as_they_should_be():
         assert (gw[0] == 3.0).all() and (gw[5] == 3.0).all()
 
 
+@pytest.mark.parametrize("dtype,Fi,Fo", [(torch.float32, 16, 40), (torch.float32, 40, 40), (torch.bfloat16, 40, 72)])
+def test_falling_offsets_and_partial_sums(dtype, Fi, Fo):
+    """Groups that overlap name more partial sums than the workspace holds: nothing behind it is read or written."""
+    m, G = 60_000, 4
+    x, d = randn(m, Fi, seed=33, dtype=dtype), randn(m, Fo, seed=34, dtype=dtype)
+    need = epp.epp_grouped_weight_gradient_workspace(m, G, Fi, Fo)
+    assert need > 4 * 8 * G * Fi * Fo  # (the entries are cut)
+    for bad in ([0, m, 0, m, m], [0, m, 0, m, 0], [0, m, 0, 2 ** 31 - 1, 7]):
+        held = torch.full((4 * need,), 255, dtype=torch.uint8, device=dev())
+        got = torch.full((G + 2, Fi, Fo), 3.0, dtype=dtype, device=dev())
+        epp.epp_grouped_weight_gradient(x, d, torch.tensor(bad, dtype=torch.int32, device=dev()), got[1:-1], held[:need])
+        assert (held[need:] == 255).all() and (got[0] == 3.0).all() and (got[-1] == 3.0).all()
+        assert torch.isfinite(got).all()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_places_past_32_bits(dtype):
     """Rows that lie more than 2^32 bytes behind the first."""

@@ -57,6 +57,23 @@ def test_weight_gradient():
             epp.epp_grouped_weight_gradient_workspace(*bad)
 
 
+def test_grouped_launches_too_large():
+    """More tiles of the result than a launch has workgroups for; offsets on memory that the weight gradient writes."""
+    lib, m = epp.load_library(), (1 << 31) - 1
+    B = 1 << 45
+
+    def many(data, ld):
+        return ctypes.byref(epp._Rows(data, m, ld, None))
+    for type_, Fi, Fo in ((0, 128, 256), (1, 16, 16), (2, 24, 1000)):
+        for fn in (lib.epp_grouped_product, lib.epp_grouped_input_gradient):
+            assert fn(type_, many(A, 1024), A, A, 2048, m, Fi, Fo, many(B, 1024), None) == LARGE
+            assert b"tiles" in lib.epp_last_error()
+    assert lib.epp_grouped_weight_gradient(0, rows(ld=65_536), rows(2 * A, ld=65_536), A, 2048, 10, 65_536, 65_536, 0, B, B // 2, 16, None) == LARGE
+    need = lib.epp_grouped_weight_gradient_workspace(10, 4, 16, 16)
+    for offsets in (4 * A, 4 * A + 4 * 1020, 5 * A, 5 * A + need - 4):
+        assert lib.epp_grouped_weight_gradient(1, rows(), rows(2 * A), offsets, 4, 10, 16, 16, 0, 4 * A, 5 * A, need, None) == BAD
+
+
 def test_group_rows():
     lib = epp.load_library()
     need = lib.epp_group_rows_workspace(10_000, 8)
