@@ -82,12 +82,11 @@ struct LinesOfK {
     unsigned off[DIRECT ? N : 1];
     const char* p[DIRECT ? 1 : N];
     uintx4 held[DIRECT ? 1 : N];
-    int shift;         // .. by so many bits, once they are here
-    bool cut;          // .. in some lanes
+    bool cut;          // .. some of them cut short
     int k, K;          // the contraction's element in this thread's pieces, and its end
     unsigned lds_wave;
-    // place(i): place of tile row i as seen from `from`, -1: none
-    template <class F> __device__ __forceinline__ void start(const char* from, int end, int wave, F place) {
+    // row_at(i): tile row i, counted from `from`, -1: none
+    template <class F> __device__ __forceinline__ void start(const char* from, int64_t pitch, int end, int wave, F row_at) {
         const int t = threadIdx.x;
         K = end;
         k = ((t % kPieces) ^ turn(t / kPieces)) * E;
@@ -95,9 +94,9 @@ struct LinesOfK {
         lds_wave = (unsigned)wave * 1024u;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int64_t at = place((i * NT + t) / kPieces);
-            if constexpr (DIRECT) off[i] = (unsigned)(at < 0 ? 0 : at) + (unsigned)k * (unsigned)sizeof(T);
-            else p[i] = at < 0 ? nullptr : from + at;
+            const int64_t r = row_at((i * NT + t) / kPieces);
+            if constexpr (DIRECT) off[i] = (unsigned)(r < 0 ? 0 : r * pitch) + (unsigned)k * (unsigned)sizeof(T);
+            else p[i] = r < 0 ? nullptr : from + r * pitch;
         }
     }
     __device__ __forceinline__ void prepare() {}
@@ -110,7 +109,6 @@ struct LinesOfK {
             else load_to_lds(k < K ? base + off[i] : zeros(), at);
         } else {
             held[i] = load_piece<T>(p[i] + (int64_t)k * (int64_t)sizeof(T), p[i] ? K - k : 0, K < E, zeros());
-            shift = shift_of<T>(K - k, K < E);
             cut = !FULL;
         }
     }
@@ -121,7 +119,7 @@ struct LinesOfK {
     __device__ __forceinline__ void put(char* to) {
         if constexpr (!DIRECT) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) *reinterpret_cast<uintx4*>(to + (i * NT + threadIdx.x) * 16) = cut ? shifted(held[i], shift) : held[i];
+            for (int i = 0; i < N; ++i) *reinterpret_cast<uintx4*>(to + (i * NT + threadIdx.x) * 16) = cut ? shifted(held[i], shift_of<T>(K - (k - kSteps), K < E)) : held[i];
         }
     }
     // Piece 2 s + half of rows c0 + l % 32 (c0 a multiple of 32).
@@ -148,7 +146,7 @@ struct LinesOfWidth {
     static constexpr int kLines = NT / kPieces;  // lines from piece to piece of a thread
     static_assert(kLines % 8 == 0, "all of a thread's pieces are of the same columns");
     Side s;
-    int64_t at, last;   // entry of this thread's first piece in the next tile, and the end
+    uint32_t at, last;  // entry of this thread's first piece in the next tile, and the end
     int c, width;       // column of this thread's pieces; columns
     const char* base;   // DIRECT, no list: place of the next tile's first line, the same for all lanes
     unsigned off;       // .. and of this thread's first piece, seen from there
@@ -161,13 +159,12 @@ struct LinesOfWidth {
     int32_t row[!DIRECT && LIST ? N : 1];
     unsigned lds_wave;
     uintx4 held[DIRECT ? 1 : N];
-    int shift;          // .. by so many bits, once they are here
-    bool cut;           // .. in some lanes
+    bool cut;           // .. some of them cut short
     __device__ __forceinline__ void start(const Side& side, int64_t first, int64_t end, int c0, int w, int wave, char* lds_ring = nullptr, bool loads_list = false) {
         const int t = threadIdx.x, line = t / kPieces;
         s = side;
-        at = first + line;
-        last = end;
+        at = (uint32_t)first + (uint32_t)line;
+        last = (uint32_t)end;
         width = w;
         c = c0 + ((t % kPieces) ^ (turn(line) << 1)) * E;
         lds_wave = (unsigned)wave * 1024u;
@@ -186,7 +183,6 @@ struct LinesOfWidth {
             ask_rows(1);
         }
         if constexpr (!DIRECT) {
-            shift = shift_of<T>(width - c, width < E);
             cut = c0 + TD > width;
             if constexpr (LIST) next_rows();
         }
@@ -196,7 +192,7 @@ struct LinesOfWidth {
     // and 2,048 x 2,048 weights.)
     __device__ __forceinline__ void ask_rows(int q) {
         if (asks) {
-            const int64_t e = ask + (threadIdx.x & 63);
+            const int64_t e = ask + (threadIdx.x & 63);  // (`ask` and `at` pass the last entry, but not 2^32)
             if (s.rows) load4_to_lds(reinterpret_cast<const char*>(e < last ? s.rows + e : &g_none), lds_address(ring) + (unsigned)q * 256u);
             else reinterpret_cast<int32_t*>(ring + q * 256)[threadIdx.x & 63] = e < last ? (int32_t)e : -1;
         }
@@ -225,12 +221,13 @@ struct LinesOfWidth {
             else if (FULL) load_to_lds(base + (int64_t)(i * kLines) * s.ld, off, lds);
             else load_to_lds(at + i * kLines < last ? base + (int64_t)(i * kLines) * s.ld + off : zeros(), lds);
         } else {
-            const int64_t e = at + i * kLines;
-            int64_t r = e;
+            const uint32_t e = at + i * kLines;
+            int64_t r = (int64_t)e;
+            bool no = e >= last || c >= width;
             if constexpr (LIST) {
                 if (s.rows) r = row[i];
+                no = no || r < 0 || r >= s.n;
             }
-            const bool no = e >= last || r < 0 || r >= s.n || c >= width;
             held[i] = load_piece<T>(s.data + r * s.ld + (int64_t)c * (int64_t)sizeof(T), no ? 0 : width - c, width < E, zeros());
         }
     }
@@ -246,7 +243,7 @@ struct LinesOfWidth {
     __device__ __forceinline__ void put(char* to) {
         if constexpr (!DIRECT) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) *reinterpret_cast<uintx4*>(to + (i * NT + threadIdx.x) * 16) = cut ? shifted(held[i], shift) : held[i];
+            for (int i = 0; i < N; ++i) *reinterpret_cast<uintx4*>(to + (i * NT + threadIdx.x) * 16) = cut ? shifted(held[i], shift_of<T>(width - c, width < E)) : held[i];
         }
     }
     // Piece 2 s + half of the contraction for columns c + l % 32.
@@ -302,11 +299,11 @@ __device__ __forceinline__ void form_tile(const GroupedArgs& g, const Place& at,
         const int64_t ldw = (int64_t)g.F_out * (int64_t)sizeof(T);
         K = MODE == kInput ? g.F_out : g.F_in;
         // (with a list a row's place is counted from the first one, else from the tile's)
-        a.start(g.a.rows ? g.a.data : g.a.data + m0 * g.a.ld, (int)K, w, [&](int i) -> int64_t {
+        a.start(g.a.rows ? g.a.data : g.a.data + m0 * g.a.ld, g.a.ld, (int)K, w, [&](int i) -> int64_t {
             const int64_t r = row_of(g.a, m0 + i, m0 + i < m_end);
-            return r < 0 ? -1 : (g.a.rows ? r : (int64_t)i) * g.a.ld;
+            return r < 0 ? -1 : g.a.rows ? r : (int64_t)i;
         });
-        if constexpr (MODE == kInput) b.start(W + n0 * ldw, (int)K, w, [&](int i) -> int64_t { return n0 + i < N ? i * ldw : -1; });
+        if constexpr (MODE == kInput) b.start(W + n0 * ldw, ldw, (int)K, w, [&](int i) -> int64_t { return n0 + i < N ? i : -1; });
         else b.start(Side{W, K, ldw, nullptr}, 0, K, n0, N, w);
     } else {
         K = at.last - at.first;
@@ -687,8 +684,10 @@ bool small_tiles(int64_t tiles) { return tiles < kUnits; }
 // 16 bits: tiles of 256 x 256, which fetch half as much a product as tiles of 128 x 128 but come one to a compute unit, where there are enough
 // of them and the width does not waste a part of each.  bfloat16, groups of exponentially distributed sizes, 128 / 256 wide, us: 2,048 entries,
 // 16 groups, 4,096 x 4,096 (about 256 tiles of 256) 173 / 154; 32,768, 32, 4,096 x 2,048 663 / 593; 32,768, 64, 2,048 x 512 (320) 112 / 101;
-// but 8,192, 64, 2,048 x 512 (128) 34 / 55, 512, 4, 4,096 x 4,096 (64) 49 / 85, and 32,768, 4, 256 x 384 (a quarter wasted) 24 / 29.
-bool large_tiles(int64_t rows, int width) { return (width % 256 == 0 || width >= 1024) && rows * ((width + 255) / 256) >= 192; }
+// 60,000, 8, 1,000 x 1,000 178 / 152; but 8,192, 64, 2,048 x 512 (128) 34 / 55, 512, 4, 4,096 x 4,096 (64) 49 / 85, and 32,768, 4, 256 x 384 (a
+// quarter wasted) 24 / 29.  Through registers the product would need more of them than there are; with tiles of 128 x 256 it took longer (532
+// / 549 for 32,768, 16, 2,047 x 2,047; its gradients 536 / 428 and, of the weights, 579 / 421).
+bool large_tiles(int64_t rows, int width) { return ((width + 255) / 256 * 2048 <= 9 * width || width >= 1024) && rows * ((width + 255) / 256) >= 192; }
 
 template <class T, int MODE>
 int launch_rows(const GroupedArgs& g, bool direct, hipStream_t s) {
@@ -697,8 +696,12 @@ int launch_rows(const GroupedArgs& g, bool direct, hipStream_t s) {
         if (narrow_rows(g.m, K, N)) return launch_narrow_rows(MODE == kInput, g, s);
     if (few_rows(sizeof(T) == 4, MODE == kInput, direct, g.m, g.G, K, N))
         return launch_few(sizeof(T) == 4 ? EPP_FLOAT32 : std::is_same_v<T, __bf16> ? EPP_BFLOAT16 : EPP_FLOAT16, MODE == kInput, direct, g, s);
-    if constexpr (sizeof(T) == 2)
-        if (direct && large_tiles(g.m / 256 + g.G / 2, N)) return launch_rows_of<T, MODE, 2, 4, 4, 2, true, true>(g, s);
+    if constexpr (sizeof(T) == 2) {
+        const bool large = large_tiles(g.m / 256 + g.G / 2, N);
+        if (direct && large) return launch_rows_of<T, MODE, 2, 4, 4, 2, true, true>(g, s);
+        if constexpr (MODE == kInput)
+            if (large) return launch_rows_of<T, MODE, 2, 4, 4, 2, false, true>(g, s);
+    }
     if (sizeof(T) == 4 || small_tiles((g.m / 128 + g.G / 2) * ((N + 127) / 128))) {
         if constexpr (sizeof(T) == 2)
             if (direct && (g.m / 64 + g.G / 2) * ((N + 63) / 64) <= kUnits) return launch_rows_of<T, MODE, 2, 2, 1, 1, true, false, 4>(g, s);
@@ -781,7 +784,8 @@ int launch_weight_of(const GroupedArgs& g, int64_t chunks, hipStream_t s) {
 template <class T, class TO>
 int launch_weight_tiles(const GroupedArgs& g, int64_t chunks, bool direct, hipStream_t s) {
     if constexpr (sizeof(T) == 2)
-        if (direct && !g.per && g.F_in >= 256 && large_tiles((int64_t)g.G * ((g.F_in + 255) / 256) / 3, g.F_out)) {
+        if (!g.per && g.F_in >= 256 && large_tiles((int64_t)g.G * ((g.F_in + 255) / 256) / 3, g.F_out)) {
+            if (!direct) return launch_weight_of<T, TO, 2, 4, 4, 2, false, true>(g, chunks, s);
             if (g.a.rows || g.b.rows) return launch_weight_of<T, TO, 2, 4, 4, 2, true, true>(g, chunks, s);
             return launch_weight_of<T, TO, 2, 4, 4, 2, true, false>(g, chunks, s);
         }

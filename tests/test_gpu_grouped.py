@@ -167,6 +167,31 @@ def test_large_tiles(dtype):
         assert_sums(got, want, size, terms)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_large_tiles_of_any_alignment(dtype):
+    """The same with rows that are no multiples of 16 bytes, and widths that all but fill their tiles."""
+    for sizes in ([700, 0, 300, 1, 255, 257, 600, 900], [513] * 9):
+        run_rows(sizes, 3_329, 131, dtype, True, 35)
+        run_rows(sizes, 3_329, 7, dtype, True, 36)  # (less than a piece)
+        run_rows(sizes, 131, 3_329, dtype, False, 37)
+        run_rows(sizes, 72, 3_320, dtype, False, 38)
+    sizes, Fi, Fo = [100, 0, 31, 300, 64, 1, 65, 100, 129, 0, 33], 1_537, 2_047
+    m, G, offsets = sum(sizes), len(sizes), offsets_of(sizes)
+    x, d = randn(m + 20, Fi, seed=39, dtype=dtype), randn(m + 7, Fo, seed=40, dtype=dtype)
+    x_rows = torch.randperm(m + 20, generator=torch.Generator().manual_seed(4))[:m].int().to(dev())
+    d_rows = torch.randint(0, m + 7, (m,), generator=torch.Generator().manual_seed(5)).int().to(dev())
+    x_rows[50], d_rows[60] = -1, 2 ** 31 - 1
+    ws = torch.empty(epp.epp_grouped_weight_gradient_workspace(m, G, Fi, Fo), dtype=torch.uint8, device=dev())
+    for to in {dtype, torch.float32}:
+        held = torch.full((G * Fi * Fo + 2,), 5.0, dtype=to, device=dev())
+        got = held[1:-1].view(G, Fi, Fo)
+        for lists in (dict(), dict(x_rows=x_rows), dict(x_rows=x_rows, grad_rows=d_rows)):
+            epp.epp_grouped_weight_gradient(x if lists else x[:m], d if len(lists) == 2 else d[:m], offsets, got, ws, **lists)
+            want, size, terms = weight_gradient(x, d, offsets, m, lists.get("x_rows"), lists.get("grad_rows"))
+            assert_sums(got, want, size, terms)
+        assert held[0] == 5.0 and held[-1] == 5.0
+
+
 def test_offsets_that_are_not_as_they_should_be():
     """Falling, negative and too large ones: unspecified results in the rows, nothing outside them."""
     x, W = randn(100, 24, seed=31, dtype=torch.bfloat16), randn(4, 24, 40, seed=32, dtype=torch.bfloat16)
