@@ -687,7 +687,16 @@ bool small_tiles(int64_t tiles) { return tiles < kUnits; }
 // 60,000, 8, 1,000 x 1,000 178 / 152; but 8,192, 64, 2,048 x 512 (128) 34 / 55, 512, 4, 4,096 x 4,096 (64) 49 / 85, and 32,768, 4, 256 x 384 (a
 // quarter wasted) 24 / 29.  Through registers the product would need more of them than there are; with tiles of 128 x 256 it took longer (532
 // / 549 for 32,768, 16, 2,047 x 2,047; its gradients 536 / 428 and, of the weights, 579 / 421).
-bool large_tiles(int64_t rows, int width) { return ((width + 255) / 256 * 2048 <= 9 * width || width >= 1024) && rows * ((width + 255) / 256) >= 192; }
+bool fills(int width) { return (width + 255) / 256 * 2048 <= 9 * width || width >= 1024; }
+bool large_tiles(int64_t rows, int width) { return fills(width) && rows * ((width + 255) / 256) >= 192; }
+// Weight gradients, whose tiles each go through all entries of a group: enough that the longest group's take at most twice as long as the
+// average compute unit's share (the longest of G exponentially distributed sizes is 1 + 1/2 + .. + 1/G, about ln G + 0.58, times their
+// average).  128 / 256 wide, us: 2 groups, 8,000 entries, 4,096 x 4,096 (512 tiles of 256) 325 / 254, 3,001 x 3,999 of 4,000 (384) 203 / 175; 4,
+// 16,000, 1,500 x 3,000 (288) 355 / 267; but 8, 16,000, 2,048 x 1,024 (256) 88 / 122; 64, 32,768, 512 x 512 (256) 56 / 90.
+bool large_weight_tiles(int G, int F_in, int F_out) {
+    const int64_t tiles = (int64_t)G * ((F_in + 255) / 256) * ((F_out + 255) / 256);
+    return F_in >= 256 && fills(F_out) && (double)tiles >= kUnits / 2 * (std::log((double)G) + 0.58);
+}
 
 template <class T, int MODE>
 int launch_rows(const GroupedArgs& g, bool direct, hipStream_t s) {
@@ -784,7 +793,7 @@ int launch_weight_of(const GroupedArgs& g, int64_t chunks, hipStream_t s) {
 template <class T, class TO>
 int launch_weight_tiles(const GroupedArgs& g, int64_t chunks, bool direct, hipStream_t s) {
     if constexpr (sizeof(T) == 2)
-        if (!g.per && g.F_in >= 256 && large_tiles((int64_t)g.G * ((g.F_in + 255) / 256) / 3, g.F_out)) {
+        if (!g.per && large_weight_tiles(g.G, g.F_in, g.F_out)) {
             if (!direct) return launch_weight_of<T, TO, 2, 4, 4, 2, false, true>(g, chunks, s);
             if (g.a.rows || g.b.rows) return launch_weight_of<T, TO, 2, 4, 4, 2, true, true>(g, chunks, s);
             return launch_weight_of<T, TO, 2, 4, 4, 2, true, false>(g, chunks, s);
