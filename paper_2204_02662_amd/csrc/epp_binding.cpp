@@ -350,10 +350,13 @@ PyObject* group_rows(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* k
         PyErr_SetString(PyExc_ValueError, "shapes: G >= 1, offsets G + 1, order as many as rows (without rows, as group_of)");
         return nullptr;
     }
+    // (what is written: a tensor that shares its memory until then gets its own)
+    int32_t* const to_offsets = THPVariable_Unpack(a[2]).mutable_data_ptr<int32_t>();
+    int32_t* const to_order = m ? THPVariable_Unpack(a[3]).mutable_data_ptr<int32_t>() : nullptr;
     if (!current_stream(&s)) return nullptr;
     int rc;
     Py_BEGIN_ALLOW_THREADS
-    rc = epp_group_rows(group_of, n_rows, rows, m, (int)G, const_cast<int32_t*>(offsets), const_cast<int32_t*>(order), ws, bytes, s);
+    rc = epp_group_rows(group_of, n_rows, rows, m, (int)G, to_offsets, to_order, ws, bytes, s);
     Py_END_ALLOW_THREADS
     return finish(rc);
 }
