@@ -233,8 +233,9 @@ c10::DeviceIndex current_device() {
     return guard->getDevice().index();
 }
 
-// A tensor on the current device; its memory is what the kernels of the current stream use.
-const at::Tensor* device_tensor(PyObject* o, const char* what) {
+// A tensor on the current device; its memory is what the kernels of the current stream use.  (any_sign: also one that stands for the
+// negative of its memory)
+const at::Tensor* device_tensor(PyObject* o, const char* what, bool any_sign = false) {
     if (!THPVariable_Check(o)) {
         PyErr_Format(PyExc_TypeError, "%s: expected a tensor, got %s", what, Py_TYPE(o)->tp_name);
         return nullptr;
@@ -250,6 +251,10 @@ const at::Tensor* device_tensor(PyObject* o, const char* what) {
         PyErr_Format(PyExc_ValueError, "%s is on %s, the current device is cuda:%d", what, on.c_str(), (int)current_device());
         return nullptr;
     }
+    if (t.is_neg() && !any_sign) {
+        PyErr_Format(PyExc_ValueError, "%s is a view that stands for the negative of its memory (resolve_neg() gives a tensor that does not)", what);
+        return nullptr;
+    }
     return &t;
 }
 
@@ -263,8 +268,8 @@ int element_type(const at::Tensor& t) {  // -1: none that the library has
 }
 
 // float32, bfloat16 or float16, of `dims` dimensions (0: any).
-const at::Tensor* numbers(PyObject* o, const char* what, int dims, int* type) {
-    const at::Tensor* t = device_tensor(o, what);
+const at::Tensor* numbers(PyObject* o, const char* what, int dims, int* type, bool any_sign = false) {
+    const at::Tensor* t = device_tensor(o, what, any_sign);
     if (!t) return nullptr;
     *type = element_type(*t);
     if (*type < 0) {
@@ -471,7 +476,7 @@ PyObject* gradients(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw
     std::vector<epp_gradient_t> grads((size_t)count);
     for (Py_ssize_t i = 0; i < count; ++i) {
         int type, type_out;
-        const at::Tensor* x = numbers(PyTuple_GET_ITEM(in.o, i), "a gradient", 0, &type);
+        const at::Tensor* x = numbers(PyTuple_GET_ITEM(in.o, i), "a gradient", 0, &type, true);
         if (!x) return nullptr;
         if (!x->is_non_overlapping_and_dense()) {
             PyErr_Format(PyExc_ValueError, "gradient %zd: its elements must fill their memory, without gaps", i);
@@ -482,10 +487,14 @@ PyObject* gradients(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw
         g.count = x->numel();
         g.out = nullptr;
         if (out.o) {
-            const at::Tensor* y = numbers(PyTuple_GET_ITEM(out.o, i), "an output", 0, &type_out);
+            const at::Tensor* y = numbers(PyTuple_GET_ITEM(out.o, i), "an output", 0, &type_out, true);
             if (!y) return nullptr;
             if (type_out != type || y->sizes() != x->sizes() || y->strides() != x->strides()) {
                 PyErr_Format(PyExc_ValueError, "output %zd: type, shape and strides must be the gradient's", i);
+                return nullptr;
+            }
+            if (y->is_neg() != x->is_neg()) {
+                PyErr_Format(PyExc_ValueError, "gradient %zd or its output is a view that stands for the negative of its memory, the other is not", i);
                 return nullptr;
             }
             g.out = y->mutable_data_ptr();

@@ -21,3 +21,34 @@ def test_group_rows_writes_to_its_own_copy(m):
     assert (offsets == -9).all() and (order == -9).all()
     assert torch.equal(lazy[1], torch.sort(group_of, stable=True).indices.int())
     assert torch.equal(lazy[0][1:], torch.bincount(group_of, minlength=G).cumsum(0).int()) and lazy[0][0] == 0
+
+
+def test_views_that_only_change_the_sign_are_refused():
+    """A tensor that stands for the negative of its memory: its numbers are not what lies there."""
+    def t(*shape, dtype=torch.float32):
+        return torch.ones(*shape, dtype=dtype, device=dev())
+    x, W, y, s = t(6, 4), t(2, 4, 4), t(6, 4), t(1)
+    offsets = torch.tensor([0, 3, 6], dtype=torch.int32, device=dev())
+    b = torch.empty(1 << 16, dtype=torch.uint8, device=dev())
+    neg = torch._neg_view
+    assert neg(x).is_neg() and neg(x).is_contiguous()
+    for call in (lambda: epp.epp_grouped_product(neg(x), W, offsets, y), lambda: epp.epp_grouped_product(x, neg(W), offsets, y),
+                 lambda: epp.epp_grouped_product(x, W, offsets, neg(y)), lambda: epp.epp_grouped_input_gradient(neg(x), W, offsets, y),
+                 lambda: epp.epp_grouped_weight_gradient(neg(x), y, offsets, W, b), lambda: epp.epp_grouped_weight_gradient(x, neg(y), offsets, W, b),
+                 lambda: epp.epp_grouped_weight_gradient(x, y, offsets, neg(W), b), lambda: epp.epp_gradient_norm([x], neg(s), b),
+                 lambda: epp.epp_clip_gradients([neg(x)], 1.0, s, b, out=[y]), lambda: epp.epp_clip_gradients([x], 1.0, s, b, out=[neg(y)])):
+        with pytest.raises(ValueError, match="negative"):
+            call()
+    # (a norm has no sign, and what is scaled in place keeps it)
+    epp.epp_gradient_norm([neg(x)], s, b)
+    assert abs(s.item() - 24 ** 0.5) <= 2.0 ** -24 * 5
+    g = neg(torch.full((8, 2), 2.0, device=dev()))
+    epp.epp_clip_gradients([g], 4.0, s, b)
+    assert s.item() == 8.0 and (g == -1.0).all()
+    # (what such a program has in hand: the imaginary part of a conjugate)
+    z = torch.full((6, 1), 1 + 2j, dtype=torch.complex64, device=dev()).conj().imag
+    assert z.is_neg()
+    with pytest.raises(ValueError, match="negative"):
+        epp.epp_grouped_product(z, t(2, 1, 4), offsets, y)
+    epp.epp_grouped_product(z.resolve_neg(), t(2, 1, 4), offsets, y)
+    assert (y == -2.0).all()
