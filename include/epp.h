@@ -355,7 +355,8 @@ typedef struct {
  *   workspace  device, at least epp_grouped_weight_gradient_workspace(...) bytes, 16-byte aligned: partial sums over blocks of
  *              entries, which a second kernel adds in a fixed order
  * 1 <= G <= 2048, 1 <= F_in, F_out <= 65,536, 0 <= m < 2^31, and a result of fewer than 2^24 tiles (64 x 64 elements of fp32, 128 x 128
- * of 16 bits, each group's own), else EPP_ERR_TOO_LARGE.  Outputs must not alias inputs (columns of one wider matrix are fine). */
+ * of 16 bits, each group's own), else EPP_ERR_TOO_LARGE.  Outputs must not alias inputs, lists and offsets among them (columns of one wider
+ * matrix are fine). */
 int epp_grouped_product(int type, const epp_rows_t* X, const void* W, const int32_t* offsets, int G, int64_t m, int F_in, int F_out,
                         const epp_rows_t* out, epp_stream_t stream);
 int epp_grouped_input_gradient(int type, const epp_rows_t* grad_out, const void* W, const int32_t* offsets, int G, int64_t m, int F_in,

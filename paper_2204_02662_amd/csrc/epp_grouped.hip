@@ -643,11 +643,13 @@ bool overlaps_block(const epp_rows_t& x, int wx, int size, const void* p, int64_
     const uintptr_t bp = reinterpret_cast<uintptr_t>(p);
     return bx < bp + (uintptr_t)bytes && bp < ex;
 }
-bool overlaps_offsets(const int32_t* offsets, int G, const void* p, int64_t bytes) {
-    const uintptr_t o = reinterpret_cast<uintptr_t>(offsets), b = reinterpret_cast<uintptr_t>(p);
-    return o < b + (uintptr_t)bytes && b < o + 4 * ((uintptr_t)G + 1);
+// A list of `count` rows or offsets (NULL: none).
+bool overlaps_list(const int32_t* list, int64_t count, const void* p, int64_t bytes) {
+    if (!list || count <= 0 || bytes <= 0) return false;
+    const uintptr_t o = reinterpret_cast<uintptr_t>(list), b = reinterpret_cast<uintptr_t>(p);
+    return o < b + (uintptr_t)bytes && b < o + 4 * (uintptr_t)count;
 }
-int aliased() { epp_set_error("matrices must not alias"); return EPP_ERR_INVALID_ARG; }
+int aliased() { epp_set_error("outputs and the workspace must not alias anything else"); return EPP_ERR_INVALID_ARG; }
 
 bool aligned(const Side& s, int width_bytes) { return (reinterpret_cast<uintptr_t>(s.data) | (uintptr_t)s.ld | (uintptr_t)width_bytes) % 16 == 0; }
 Side side(const epp_rows_t& x, int size) { return {static_cast<const char*>(x.data), x.n, x.ld * size, x.rows}; }
@@ -734,7 +736,8 @@ int grouped_rows(int mode, int type, const epp_rows_t* in, const void* W, const 
     if (!W || !offsets) { epp_set_error("NULL argument"); return EPP_ERR_INVALID_ARG; }
     if (reinterpret_cast<uintptr_t>(W) % (unsigned)size || reinterpret_cast<uintptr_t>(offsets) % 4) { epp_set_error("address not aligned to its elements"); return EPP_ERR_INVALID_ARG; }
     if (overlap(*in, w_in, *out, w_out, size) || overlaps_block(*out, w_out, size, W, (int64_t)G * F_in * F_out * size) ||
-        overlaps_block(*out, w_out, size, offsets, 4 * ((int64_t)G + 1)))
+        overlaps_block(*out, w_out, size, offsets, 4 * ((int64_t)G + 1)) ||
+        (in->rows && overlaps_block(*out, w_out, size, in->rows, 4 * m)) || (out->rows && overlaps_block(*out, w_out, size, out->rows, 4 * m)))
         return aliased();
     if (m == 0) return EPP_OK;
     GroupedArgs g = {};
@@ -880,7 +883,9 @@ extern "C" int epp_grouped_weight_gradient(int type, const epp_rows_t* X, const 
         overlaps_block(*X, F_in, size, workspace, need) || overlaps_block(*grad_out, F_out, size, workspace, need) ||
         (reinterpret_cast<uintptr_t>(workspace) < reinterpret_cast<uintptr_t>(grad_W) + (uintptr_t)w_bytes &&
          reinterpret_cast<uintptr_t>(grad_W) < reinterpret_cast<uintptr_t>(workspace) + (uintptr_t)need) ||
-        overlaps_offsets(offsets, G, grad_W, w_bytes) || overlaps_offsets(offsets, G, workspace, need))
+        overlaps_list(offsets, (int64_t)G + 1, grad_W, w_bytes) || overlaps_list(offsets, (int64_t)G + 1, workspace, need) ||
+        overlaps_list(X->rows, m, grad_W, w_bytes) || overlaps_list(X->rows, m, workspace, need) ||
+        overlaps_list(grad_out->rows, m, grad_W, w_bytes) || overlaps_list(grad_out->rows, m, workspace, need))
         return aliased();
     GroupedArgs g = {};
     g.a = side(*X, size);
