@@ -35,6 +35,7 @@
 using namespace epp_grouped;
 
 #include <cmath>
+#include <numeric>
 
 namespace {
 
@@ -631,8 +632,9 @@ bool overlap(const epp_rows_t& x, int wx, const epp_rows_t& y, int wy, int size)
     const uintptr_t bx = reinterpret_cast<uintptr_t>(x.data), by = reinterpret_cast<uintptr_t>(y.data);
     const uintptr_t ex = bx + (uintptr_t)((x.n - 1) * x.ld + wx) * (uintptr_t)size, ey = by + (uintptr_t)((y.n - 1) * y.ld + wy) * (uintptr_t)size;
     if (ex <= by || ey <= bx) return false;
-    if (x.ld != y.ld) return true;
-    const uintptr_t pitch = (uintptr_t)x.ld * (uintptr_t)size;
+    // (every row of either begins a multiple of `pitch` behind its first: the common divisor of their distances, of which a single row has none)
+    const uintptr_t pitch = std::gcd(x.n > 1 ? (uintptr_t)x.ld : 0, y.n > 1 ? (uintptr_t)y.ld : 0) * (uintptr_t)size;
+    if (!pitch) return true;
     const uintptr_t lx = (uintptr_t)wx * (uintptr_t)size, ly = (uintptr_t)wy * (uintptr_t)size;
     const uintptr_t d = (by >= bx ? by - bx : pitch - (bx - by) % pitch) % pitch;  // y's first column, seen from x's
     return !(d >= lx && d + ly <= pitch);

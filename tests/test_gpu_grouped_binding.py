@@ -52,3 +52,17 @@ def test_views_that_only_change_the_sign_are_refused():
         epp.epp_grouped_product(z, t(2, 1, 4), offsets, y)
     epp.epp_grouped_product(z.resolve_neg(), t(2, 1, 4), offsets, y)
     assert (y == -2.0).all()
+
+
+def test_a_row_beside_the_results():
+    """The only row of the input, and every second row, in other columns of the matrix that the results are columns of."""
+    F, n = 24, 10
+    W = torch.randint(-2, 3, (2, F, F), generator=torch.Generator().manual_seed(2)).float().to(dev())
+    offsets = torch.tensor([0, 4, n], dtype=torch.int32, device=dev())
+    wide = torch.randint(-2, 3, (n, 2 * F), generator=torch.Generator().manual_seed(3)).float().to(dev())
+    for part, rows in ((slice(3, 4), [0] * n), (slice(0, n, 2), [i // 2 for i in range(n)])):
+        was, x = wide.clone(), wide[part, :F]
+        picked = was[part, :F][rows]
+        epp.epp_grouped_product(x, W, offsets, wide[:, F:], in_rows=torch.tensor(rows, dtype=torch.int32, device=dev()))
+        assert torch.equal(wide[:, :F], was[:, :F])
+        assert torch.equal(wide[:, F:], torch.cat([picked[:4] @ W[0], picked[4:] @ W[1]]))

@@ -37,3 +37,37 @@ def test_weight_gradients_on_lists_of_rows():
         assert rc(x_list=at) == BAD and b"alias" in lib.epp_last_error()
         assert rc(d_list=at) == BAD and b"alias" in lib.epp_last_error()
         assert rc(x_list=6 * A, d_list=at) == BAD
+
+
+@pytest.mark.parametrize("call", ["epp_grouped_product", "epp_grouped_input_gradient"])
+def test_columns_of_one_wider_matrix(call):
+    """10 rows of 32 floats at A: inputs in the first 16 columns, outputs in the last 16, all rows, one of them or every second one."""
+    fn = getattr(epp.load_library(), call)
+
+    def rc(x, out):
+        return fn(0, x, 2 * A, 3 * A, 4, 0, 16, 16, out, None)
+    row = 4 * 32
+    for first, second in ((A, A + 64), (A + 64, A)):  # columns of the one and of the other
+        for step in (1, 2, 3):
+            for other in (1, 2, 3):
+                assert rc(rows(first, n=10 // step, ld=32 * step), rows(second, n=10 // other, ld=32 * other)) == OK
+        for at in (0, 3, 9):
+            # (a single row may have any distance from row to row)
+            for ld in (16, 32, 1000):
+                assert rc(rows(first + at * row, n=1, ld=ld), rows(second, ld=32)) == OK
+                assert rc(rows(first, ld=32), rows(second + at * row, n=1, ld=ld)) == OK
+    # a column too many, to either side; the same columns; single rows that share an element
+    for at in (0, 3, 9):
+        for off in (60, -60, 0, 4):
+            if at * row + off < 0 or (off > 0 and at == 9):
+                continue
+            for ld in (16, 32):
+                assert rc(rows(A + at * row + off, n=1, ld=ld), rows(A, ld=32)) == BAD
+                assert rc(rows(A, ld=32), rows(A + at * row + off, n=1, ld=ld)) == BAD
+        assert rc(rows(A + at * row, n=1), rows(A + at * row + 60, n=1)) == BAD
+    assert rc(rows(A, n=5, ld=64), rows(A + 60, ld=32)) == BAD
+    assert rc(rows(A, n=5, ld=64), rows(A + 68, ld=32)) == BAD
+    assert rc(rows(A, n=3, ld=48), rows(A + 64, ld=32)) == BAD  # (its second row lies in the other's last columns)
+    # a single row wider than the distance of the other's rows
+    F_in, F_out = (64, 16) if call == "epp_grouped_product" else (16, 64)
+    assert fn(0, rows(A, n=1, ld=64), 2 * A, 3 * A, 4, 0, F_in, F_out, rows(A + 64, n=3, ld=32), None) == BAD
