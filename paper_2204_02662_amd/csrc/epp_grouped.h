@@ -96,13 +96,20 @@ __device__ __forceinline__ unsigned lds_address(const void* p) {
     return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 // 16 bytes a lane into LDS, lane after lane from `to` on.  Complete once vmcnt says so (wait_and_meet).  (Not the compiler's builtin: it waits
-// for all of these loads before every transposing LDS read, those of the next tile included.  The compiler writes m0 right before its own uses.)
+// for all of these loads before every transposing LDS read, those of the next tile included.  m0 is named as
+// changed, of which the compiler warns that it is a register that it reserves: it keeps values there from one of its own uses to the next.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(const char* from, unsigned to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
 }
 __device__ __forceinline__ void load_to_lds(const char* base, unsigned off, unsigned to) {  // (base the same in all lanes)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
 }
+__device__ __forceinline__ void load4_to_lds(const char* from, unsigned to) {  // (4 bytes a lane)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+}
+#pragma clang diagnostic pop
 
 // Between a wavefront's own writes to LDS and reads by other lanes of it, both ways: LDS serves them in order, and the compiler keeps it.
 __device__ __forceinline__ void in_order() {

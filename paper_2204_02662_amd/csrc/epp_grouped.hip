@@ -62,9 +62,6 @@ __device__ __forceinline__ floatx16 multiply(uintx4 a, uintx4 b, floatx16 c) {
 }
 
 // ---------------------------------------------------------------- operand tiles
-__device__ __forceinline__ void load4_to_lds(const char* from, unsigned to) {  // (4 bytes a lane)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory");
-}
 // All loads of this wavefront have arrived and all its LDS reads are done; then the same for the workgroup's.
 // (ALLOWED: but for the last so many loads)
 template <int ALLOWED>
