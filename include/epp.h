@@ -385,8 +385,8 @@ typedef struct {
  *   norm       device, one float
  *   workspace  device, at least epp_gradient_norm_workspace(n) bytes, 16-byte aligned
  * What is written must not overlap with anything else: a gradient listed twice is refused by epp_clip_gradients (and counts twice in
- * epp_gradient_norm).  Enqueues only: one launch for the norm of up to 96 gradients and one to
- * finish or to scale, or a single one for gradients of few elements (about 32 times 1,024). */
+ * epp_gradient_norm).  Enqueues only: for every 96 gradients one launch for the norm and (epp_clip_gradients) one to scale, and at most one that
+ * adds up what the launches found; a single one for gradients of few elements (about 32 times 1,024). */
 int64_t epp_gradient_norm_workspace(int n); /* bytes, < 0: error */
 int epp_gradient_norm(const epp_gradient_t* grads, int n, float* norm, void* workspace, int64_t workspace_bytes, epp_stream_t stream);
 int epp_clip_gradients(const epp_gradient_t* grads, int n, double max_norm, float* norm, void* workspace, int64_t workspace_bytes,
