@@ -218,11 +218,17 @@ int launch_of(const GroupedArgs& g, hipStream_t s) {
     return EPP_OK;
 }
 
+// Whether these kernels serve few rows however many tiles of 128 columns there are.
+constexpr bool always(bool fp32, bool input, bool direct) { return fp32 && (direct || !input); }
+
 template <class T, int MODE, int R, bool DIRECT>
 int launch_columns(const GroupedArgs& g, hipStream_t s) {
-    const int N = MODE == kInput ? g.F_in : g.F_out;
-    const int64_t groups = std::min<int64_t>(g.G, g.m);
-    if (groups * ((N + 63) / 64) >= 2 * kUnits) return launch_of<T, MODE, R, 64, DIRECT>(g, s);
+    // (where few_rows leaves 2 kUnits of the wider tiles to these kernels)
+    if constexpr (always(sizeof(T) == 4, MODE == kInput, DIRECT)) {
+        const int N = MODE == kInput ? g.F_in : g.F_out;
+        const int64_t groups = std::min<int64_t>(g.G, g.m);
+        if (groups * ((N + 63) / 64) >= 2 * kUnits) return launch_of<T, MODE, R, 64, DIRECT>(g, s);
+    }
     return launch_of<T, MODE, R, 32, DIRECT>(g, s);
 }
 
@@ -252,7 +258,7 @@ int launch_type(bool input, bool direct, const GroupedArgs& g, hipStream_t s) {
 bool epp_grouped::few_rows(bool fp32, bool input, bool direct, int64_t m, int G, int K, int N) {
     if (std::min(K, N) < 8) return false;  // (rows shorter than a piece)
     if (m >= (fp32 ? 24 : 32) * (int64_t)G) return false;
-    return (fp32 && (direct || !input)) || std::min<int64_t>(G, m) * ((N + 127) / 128) < kUnits;
+    return always(fp32, input, direct) || std::min<int64_t>(G, m) * ((N + 127) / 128) < kUnits;
 }
 
 int epp_grouped::launch_few(int type, bool input, bool direct, const GroupedArgs& g, hipStream_t s) {

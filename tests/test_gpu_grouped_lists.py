@@ -116,6 +116,17 @@ def test_few_rows(dtype, step, lists):
 
 
 @pytest.mark.parametrize("lists", LISTS)
+@pytest.mark.parametrize("step", [8, 3])
+def test_few_rows_of_many_groups(step, lists):
+    """Floats: 72 groups times 17 blocks of 64 columns."""
+    for per in (5, 17):
+        sizes = [(per * i) % (2 * per) + i % 3 for i in range(72)]
+        run_rows(sizes, 264, 1_032, torch.float32, False, 35, step, *lists)
+        run_rows(sizes, 1_032, 264, torch.float32, True, 36, step, *lists)
+        run_rows(sizes, 133, 1_025, torch.float32, False, 37, step, *lists)
+
+
+@pytest.mark.parametrize("lists", LISTS)
 @pytest.mark.parametrize("Fi,Fo", [(16, 41), (41, 16), (128, 30), (7, 100), (32, 32), (1, 128), (64, 47), (97, 66)])
 def test_narrow_floats(Fi, Fo, lists):
     """From 49,152 entries on where a side is at most 32, else from 2^19."""
