@@ -337,7 +337,7 @@ typedef struct {
     int64_t n;           /* rows, < 2^31                                                         */
     int64_t ld;          /* elements from row to row, at least the width                         */
     const int32_t* rows; /* device, m; a row outside [0, n) counts as zeros and is never written
-                            (times a weight that is infinite or NaN: zero or NaN) */
+                            (times an infinity or a NaN of the other matrix: zero or NaN) */
 } epp_rows_t;
 
 /* Products of a layer with a weight matrix per group, entry i in group g:

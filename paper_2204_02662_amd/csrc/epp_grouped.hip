@@ -26,8 +26,8 @@
 // Sums are fp32; 16-bit results are rounded once, when they are written.
 //
 // What bounds them: large tiles of 16 bits the matrix cores together with what feeds them.  8,192 x 2,048 weights, 32 groups of 1,024
-// entries in bfloat16 run at 1,170 TFLOP/s (a library product of that size 1,290; these kernels without their loads of operands 1,430);
-// groups of uneven sizes lose another eighth to rows that are not there.  Floats: 129 of the matrix cores' 157 TFLOP/s.  The weight gradient
+// entries in bfloat16 run at 1,160 TFLOP/s (a library product of 8,192 x 4,096 x 2,048 1,300; these kernels without most of their loads of
+// operands 1,490); groups of exponentially distributed sizes at 960.  Floats: 122 to 128 TFLOP/s (a library product 153).  The weight gradient
 // writes more than the products do: 256 KB a tile of floats, which nothing else in the compute unit overlaps.
 
 #include "epp_grouped.h"
@@ -693,7 +693,10 @@ bool large_tiles(int64_t rows, int width) { return fills(width) && rows * ((widt
 // Weight gradients, whose tiles each go through all entries of a group: enough that the longest group's take at most twice as long as the
 // average compute unit's share (the longest of G exponentially distributed sizes is 1 + 1/2 + .. + 1/G, about ln G + 0.58, times their
 // average).  128 / 256 wide, us: 2 groups, 8,000 entries, 4,096 x 4,096 (512 tiles of 256) 325 / 254, 3,001 x 3,999 of 4,000 (384) 203 / 175; 4,
-// 16,000, 1,500 x 3,000 (288) 355 / 267; but 8, 16,000, 2,048 x 1,024 (256) 88 / 122; 64, 32,768, 512 x 512 (256) 56 / 90.
+// 16,000, 1,500 x 3,000 (288) 355 / 267; but 8, 16,000, 2,048 x 1,024 (256) 88 / 122; 64, 32,768, 512 x 512 (256) 56 / 90.  Below the rule's
+// bound groups of one size would gain what others lose more of, and the host knows no sizes.  Even / exponentially distributed sizes, 128 wide
+// and 256: 8, 16,000, 2,048 x 1,024 77 / 81 and 69 / 147; 64, 32,768, 512 x 512 40 / 48 and 34 / 55; 16, 16,384, 1,024 x 1,024 (256) 54 / 68 and
+// 42 / 89; above it 16, 32,768, 2,048 x 2,048 (1,024) 333 / 359 and 275 / 278; 8, 16,384, 2,048 x 2,048 (512) 143 / 151 and 132 / 166.
 bool large_weight_tiles(int G, int F_in, int F_out) {
     const int64_t tiles = (int64_t)G * ((F_in + 255) / 256) * ((F_out + 255) / 256);
     return F_in >= 256 && fills(F_out) && (double)tiles >= kUnits / 2 * (std::log((double)G) + 0.58);
